@@ -154,6 +154,26 @@ w4a8_status w4a8_rmsnorm_quantize_act(const uint16_t* x, const uint16_t* gamma, 
                                       int8_t* x_q, float* x_scale, hipStream_t stream);
 
 /*
+ * The same prologue with the residual stream's addition in front of it: what
+ * a decoder layer does between a projection's output and the next norm.
+ *     sum[m,k] = bf16(x[m,k] + residual[m,k])   (one fp32 addition, rounded
+ *                                                to nearest even)
+ * and codes and scales are those of w4a8_rmsnorm_quantize_act(sum, ...), bit
+ * for bit.
+ *   x, residual  device, bf16 bit patterns [M][K], finite, 16-byte aligned
+ *   sum          device, bf16 [M][K], 16-byte aligned: the new residual
+ *                stream.  It may be x or residual itself (in place), and
+ *                must not overlap them otherwise
+ *   gamma, eps, M, K, x_q, x_scale  as for w4a8_rmsnorm_quantize_act; x_q,
+ *                x_scale and sum must not overlap each other or an input
+ *                (W4A8_EINVAL)
+ * The sums must be finite.  Does not synchronize; deterministic.
+ */
+w4a8_status w4a8_add_rmsnorm_quantize_act(const uint16_t* x, const uint16_t* residual, const uint16_t* gamma, float eps,
+                                          int64_t M, int64_t K, uint16_t* sum, int8_t* x_q, float* x_scale,
+                                          hipStream_t stream);
+
+/*
  * Streaming prefill attention with pre-RoPE cached keys (FlashDrive, Sec.
  * 3.1 and Fig. 3).  As the window of camera frames advances, the arriving
  * frame's tokens take the last frame position of each view, in a cache
@@ -204,6 +224,129 @@ w4a8_status w4a8_stream_attention(const uint16_t* q, const uint16_t* k, const ui
 /* Workspace bytes w4a8_stream_attention needs (0 for shapes it rejects;
  * every accepted shape needs some: the rotated keys). */
 size_t w4a8_stream_attention_workspace_bytes(int64_t H, int64_t Nq, int64_t Nk);
+
+/*
+ * The 8-bit key/value cache of decoding and draft verification.  Sequences
+ * hold their tokens in blocks of W4A8_CACHE_BLOCK (64); a block is a page of
+ * a pool, named by a table.  For each kv head a page holds int8 codes of the
+ * keys and of the values and one fp32 scale for either:
+ *     s = max |x| / 127 over the block's tokens (0 where that is below 2^-90),
+ *     code = round_half_even(x / s) (0 where s = 0; tokens not there yet: 0),
+ * fp32 IEEE operations as in w4a8_quantize_act; x is the value in bf16, or the
+ * key rotated at its position (rotate-half with the caller's tables, fp32
+ * operations, rounded to bf16, as in w4a8_stream_attention).  A block that is
+ * not full is quantized anew by each append, from the exact values: a ring
+ * keeps those of each sequence's last two blocks.  So the codes do not depend
+ * on how many tokens came at a time, and tokens can be taken back (a draft's
+ * rejected ones) by appending again after a smaller length, down to 64 tokens
+ * below the greatest length that the sequence had.
+ *   k_codes, v_codes  device, int8 [n_pages][Hkv][64][128] (token by d) and
+ *                [n_pages][Hkv][128][64] (d by token), 16-byte aligned
+ *   scales       device, fp32 [n_pages][Hkv][2]: keys', values'; 8-byte aligned
+ *   k_recent, v_recent  device, bf16 [n_slots][Hkv][128][128], 16-byte
+ *                aligned: token t of the sequence with this slot in row t % 128
+ *                (read and written by the append alone)
+ */
+#define W4A8_CACHE_BLOCK 64
+#define W4A8_CACHE_RECENT 128
+typedef struct {
+  int8_t* k_codes;
+  int8_t* v_codes;
+  float* scales;
+  int64_t n_pages, Hkv;
+  uint16_t* k_recent;
+  uint16_t* v_recent;
+  int64_t n_slots;
+} w4a8_cache;
+
+/*
+ * The batch of a step, the same for the append and the attention of every
+ * layer.  The step's new tokens are rows [0, T) of a token-major matrix:
+ *   starts       device, int32 [B + 1]: rows starts[b] .. starts[b + 1] - 1 are
+ *                the new tokens of sequence b, in order (any number, also
+ *                none); not decreasing, within [0, T].  Rows of no sequence
+ *                are neither read nor written
+ *   lengths      device, int32 [B]: the tokens that a sequence holds, its new
+ *                ones included as the last of them
+ *   table        device, int32 [B][max_blocks]: the page of each of a
+ *                sequence's blocks; entries past its length are not read
+ *   pos          device, int32 [T]: the new tokens' positions in the tables
+ *                (clamped to [0, n_pos))
+ *   rope_cos, rope_sin  device, fp32 [n_pos][64], 16-byte aligned
+ *   B, T         0 <= B <= 65536, 0 <= T <= W4A8_M_MAX (either 0: a no-op)
+ *   max_blocks   1 .. 2^24;  n_pos 1 .. 2^30
+ * The arrays are read by the kernels: a captured graph's replays see what
+ * they hold then.  Values out of range reach no memory outside the buffers:
+ * starts and lengths are clamped, a block whose page is outside [0, n_pages)
+ * is not written and its tokens are seen by no query, and a sequence whose
+ * slot is outside [0, n_slots) has no ring.
+ */
+typedef struct {
+  const int32_t* starts;
+  const int32_t* lengths;
+  const int32_t* table;
+  int64_t max_blocks, B, T;
+  const int32_t* pos;
+  const float* rope_cos;
+  const float* rope_sin;
+  int64_t n_pos;
+} w4a8_batch;
+
+/*
+ * Appends the batch's new keys and values: codes and scales of every block
+ * that has a new token, and the rings.
+ *   k, v         device, bf16, 16-byte aligned: token t, kv head h at t * k_row
+ *                + h * k_head elements, 128 in a row; strides in multiples of
+ *                8 (views of a fused projection's output).  Finite: a block
+ *                with another value gets unspecified codes and scales
+ *   slots        device, int32 [B]: the ring of each sequence, or NULL
+ *                (sequence b has ring b)
+ * Every sequence of a call needs pages (of the blocks that it writes) and a
+ * ring of its own.  Hkv <= 4096, n_pages and n_slots below 2^31.  Does not synchronize;
+ * enqueues one kernel; deterministic.
+ */
+w4a8_status w4a8_cache_append(const w4a8_cache* cache, const w4a8_batch* batch, const uint16_t* k, int64_t k_row,
+                              int64_t k_head, const uint16_t* v, int64_t v_row, int64_t v_head, const int32_t* slots,
+                              hipStream_t stream);
+
+/*
+ * The new tokens' attention over the cache, in which they are already: for
+ * each query head h and new token i of a sequence with n new tokens and
+ * length L,
+ *     o[i][h] = sum_j softmax_j(scale * RoPE(q[i][h], pos[i]) . k[j]) v[j]
+ * over its tokens j <= L - n + i, with k and v the values that the cache's
+ * codes stand for and h' = h / (H / Hkv) the kv head.  A token that sees
+ * nothing gets 0.  Decoding is n = 1, draft verification a few tokens, a
+ * prompt's chunk any number, and a batch may mix them.
+ *   The rotated query is held in 16 bits relative to its largest element
+ *   (half a step is 2^-16 of it) and its products with the codes are exact
+ *   integers; softmax and sums run in fp32, the softmax weights are rounded to
+ *   fp16 (2^-11 relative) for the product with the values; the output is
+ *   rounded to bf16.
+ *   q            device, bf16: token t, head h at t * q_row + h * q_head
+ *                elements (as k above)
+ *   H            H % Hkv == 0, H <= 4096
+ *   scale        finite, of either sign or 0
+ *   max_len      an upper bound of the lengths, 1 .. 64 max_blocks: it decides
+ *                how the work is split, and bounds nothing else
+ *   o            device, bf16: token t, head h at t * o_row + h * o_head
+ *                elements; the rows must not overlap each other (W4A8_EINVAL)
+ *                or an input
+ *   workspace    device, >= w4a8_cache_attention_workspace_bytes(...) bytes,
+ *                256-byte aligned (may be NULL if that is 0): partial results
+ *                past the first 64 KiB, which this call leaves untouched, so
+ *                that it may share one buffer with the other calls' workspace;
+ *                concurrent calls must not share it
+ * Of the cache only codes and scales are read; rings may be NULL.  Does not
+ * synchronize; enqueues kernels only; deterministic.
+ */
+w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batch, const uint16_t* q, int64_t q_row,
+                                 int64_t q_head, int64_t H, float scale, int64_t max_len, uint16_t* o, int64_t o_row,
+                                 int64_t o_head, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes w4a8_cache_attention needs (0 if none, and 0 for shapes it
+ * rejects). */
+size_t w4a8_cache_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hkv, int64_t max_len);
 
 /*
  * Bytes of device workspace w4a8_linear needs for this problem (0 if none).

@@ -279,6 +279,60 @@ def streaming_attention(q_bits, k_bits, v_bits, pos_q, pos_k, cos_t, sin_t, scal
     return o64, bnd
 
 
+def add_rmsnorm_quantize(x_bits, res_bits, gamma_bits, eps):
+    """The residual stream's addition in front of rmsnorm_quantize:
+    sum = bf16(x + residual), one fp32 addition and one rounding, then
+    rmsnorm_quantize of the sum.  Returns (q, s, sum bits)."""
+    total = _bf16_round(_f32(x_bits) + _f32(res_bits))
+    q, s, _, _ = rmsnorm_quantize(total, gamma_bits, eps)
+    return q, s, total
+
+
+def cache_block(x_bits):
+    """Codes and scale of one block of the 8-bit cache for one kv head:
+    bf16 x [t][D], the tokens that the block holds.  s = max |x| / 127 in
+    fp32, 0 below 2^-90; codes round_half_even(x / s) of the fp32 quotient, 0
+    where s is 0.  Returns (codes int8 [t][D], s)."""
+    x = _f32(x_bits)
+    a = np.float32(np.max(np.abs(x))) if x.size else np.float32(0)
+    if a < np.float32(2.0 ** -90):
+        return np.zeros(x.shape, np.int8), np.float32(0)
+    s = np.float32(a / np.float32(127.0))
+    return np.rint(x / s).astype(np.int8), s
+
+
+def cache_attention(q_bits, pos, k, v, cos_t, sin_t, scale, first):
+    """Attention of a sequence's new tokens over its cache: q [n][H][D] bf16
+    bit patterns at positions pos [n], k and v fp64 [Hkv][L][D] (the values
+    that the codes stand for; k is rotated already); new token i sees keys
+    j <= first + i (none where that is negative: its output is 0).  Rotation
+    with the fp32 tables, scores, softmax and sum in fp64; nothing is rounded.
+    Returns (o [n][H][D], bnd = sum_j P_ij |v_jd|, the largest |rotated q|
+    [n][H], top = the number of keys seen times max_j P_ij max_d |v_jd| over
+    j's block of 64, [n][H])."""
+    n, H, D = q_bits.shape
+    Hkv, L, _ = k.shape
+    h2 = D // 2
+    q = _f32(q_bits).astype(np.float64)
+    c, s = cos_t[pos].astype(np.float64)[:, None], sin_t[pos].astype(np.float64)[:, None]
+    q = np.concatenate([q[..., :h2] * c - q[..., h2:] * s, q[..., h2:] * c + q[..., :h2] * s], -1)
+    o, bnd, top = np.zeros((n, H, D)), np.zeros((n, H, D)), np.zeros((n, H))
+    block = np.arange(L) // 64
+    seen = np.arange(L)[None, :] <= (first + np.arange(n))[:, None]
+    some = seen.any(axis=1)
+    if some.any():
+        for h in range(H):
+            kk, vv = k[h // (H // Hkv)], v[h // (H // Hkv)]
+            x = np.where(seen[some], (q[some, h] @ kk.T) * float(scale), -np.inf)
+            p = np.exp(x - x.max(axis=1, keepdims=True))
+            p /= p.sum(axis=1, keepdims=True)
+            o[some, h], bnd[some, h] = p @ vv, p @ np.abs(vv)
+            vmax = np.zeros(-(-L // 64))
+            np.maximum.at(vmax, block, np.abs(vv).max(axis=1))
+            top[some, h] = seen[some].sum(axis=1) * (p * vmax[block]).max(axis=1)
+    return o, bnd, np.abs(q).max(axis=-1), top
+
+
 def rope_tables(P, D, base=10000.0):
     """fp32 cos / sin tables [P][D/2] for angle p * base^(-2i/D), from fp64."""
     i = np.arange(D // 2, dtype=np.float64)

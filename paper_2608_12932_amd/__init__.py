@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -31,10 +32,24 @@ EXPORTS = ("w4a8_status_string", "w4a8_packed_weight_bytes", "w4a8_pack_weights"
            "w4a8_linear_describe", "w4a8_linear_swiglu", "w4a8_linear_swiglu_workspace_bytes",
            "w4a8_linear_swiglu_describe", "w4a8_rmsnorm_quantize_act", "w4a8_stream_attention",
            "w4a8_stream_attention_workspace_bytes", "w4a8_flow_schedule", "w4a8_flow_step",
-           "w4a8_linear_noalloc")
+           "w4a8_linear_noalloc", "w4a8_add_rmsnorm_quantize_act", "w4a8_cache_append",
+           "w4a8_cache_attention", "w4a8_cache_attention_workspace_bytes")
+CACHE_BLOCK, CACHE_RECENT, HEAD_DIM = 64, 128, 128
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 _OUT_DTYPE = {OUT_BF16: torch.bfloat16, OUT_F32: torch.float32, OUT_I32_ACC: torch.int32}
+
+
+class _CacheArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "scales")] + [
+        ("n_pages", ctypes.c_int64), ("Hkv", ctypes.c_int64), ("k_recent", ctypes.c_void_p),
+        ("v_recent", ctypes.c_void_p), ("n_slots", ctypes.c_int64)]
+
+
+class _BatchArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("starts", "lengths", "table")] + [
+        (n, ctypes.c_int64) for n in ("max_blocks", "B", "T")] + [
+        (n, ctypes.c_void_p) for n in ("pos", "rope_cos", "rope_sin")] + [("n_pos", ctypes.c_int64)]
 
 
 class W4A8Error(RuntimeError):
@@ -91,6 +106,15 @@ def lib() -> ctypes.CDLL:
         L.w4a8_flow_schedule.restype = I
         L.w4a8_flow_step.argtypes = [P, P, P, I64, I64, ctypes.c_float, I64, P, P]
         L.w4a8_flow_step.restype = I
+        L.w4a8_add_rmsnorm_quantize_act.argtypes = [P, P, P, ctypes.c_float, I64, I64, P, P, P, P]
+        L.w4a8_add_rmsnorm_quantize_act.restype = I
+        C, B = ctypes.POINTER(_CacheArgs), ctypes.POINTER(_BatchArgs)
+        L.w4a8_cache_append.argtypes = [C, B, P, I64, I64, P, I64, I64, P, P]
+        L.w4a8_cache_append.restype = I
+        L.w4a8_cache_attention.argtypes = [C, B, P, I64, I64, I64, ctypes.c_float, I64, P, I64, I64, P, SZ, P]
+        L.w4a8_cache_attention.restype = I
+        L.w4a8_cache_attention_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
+        L.w4a8_cache_attention_workspace_bytes.restype = SZ
         L.w4a8_linear_workspace_bytes.argtypes = [I64, I64, I64, I, I]
         L.w4a8_linear_workspace_bytes.restype = SZ
         L.w4a8_linear.argtypes = [P, I, P, I64, I64, P, P, I, I64, P, I, P, SZ, P]
@@ -126,6 +150,21 @@ def _alloc_on(stream):
     is not torch's current one, so that the caching allocator orders their
     reuse after the call's kernels."""
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+@contextlib.contextmanager
+def _call_on(stream, first: torch.Tensor, **others):
+    """Context of a call on tensors of first's device, which need not be the
+    current one: that device and the call's stream are current inside, for
+    allocations and launches.  Yields the stream."""
+    for name, t in others.items():
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{name} is on {t.device}, the call's first tensor on {first.device}")
+    if stream is not None and stream.device != first.device:
+        raise ValueError(f"stream is of {stream.device}, the tensors are on {first.device}")
+    s = torch.cuda.current_stream(first.device) if stream is None else stream
+    with torch.cuda.device(first.device), torch.cuda.stream(s):
+        yield s
 
 
 def _dev(t: torch.Tensor, name: str, dtype: torch.dtype) -> int:
@@ -199,6 +238,30 @@ def w4a8_rmsnorm_quantize_act(x: torch.Tensor, gamma: torch.Tensor, eps: float, 
     rc = lib().w4a8_rmsnorm_quantize_act(x_ptr, g_ptr, float(eps), M, K, q.data_ptr(), s.data_ptr(), _stream(stream))
     _check(rc, "w4a8_rmsnorm_quantize_act")
     return q, s
+
+
+def w4a8_add_rmsnorm_quantize_act(x: torch.Tensor, residual: torch.Tensor, gamma: torch.Tensor, eps: float,
+                                  out: torch.Tensor | None = None, stream=None):
+    """The residual stream's addition in front of w4a8_rmsnorm_quantize_act:
+    sum = bf16(x + residual) for bf16 x, residual [M][K] -> (codes int8
+    [M][K], scales fp32 [M], sum bf16 [M][K]).  `out` takes the sum and may be
+    x or residual itself."""
+    M, K = x.shape
+    x_ptr, r_ptr = _dev(x, "x", torch.bfloat16), _dev(residual, "residual", torch.bfloat16)
+    g_ptr = _dev(gamma, "gamma", torch.bfloat16)
+    if tuple(residual.shape) != (M, K) or tuple(gamma.shape) != (K,):
+        raise ValueError(f"residual must be [{M}][{K}] and gamma [{K}]")
+    if out is not None and tuple(out.shape) != (M, K):
+        raise ValueError(f"out must be [{M}][{K}]")
+    with _call_on(stream, x, residual=residual, gamma=gamma, out=out) as s:
+        if out is None:
+            out = torch.empty_like(x)
+        q = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        sc = torch.empty((M,), dtype=torch.float32, device=x.device)
+        rc = lib().w4a8_add_rmsnorm_quantize_act(x_ptr, r_ptr, g_ptr, float(eps), M, K, _dev(out, "out", torch.bfloat16),
+                                                 q.data_ptr(), sc.data_ptr(), s.cuda_stream)
+    _check(rc, "w4a8_add_rmsnorm_quantize_act")
+    return q, sc, out
 
 
 def w4a8_flow_schedule(n_steps: int, n_reuse: int) -> list:
@@ -463,3 +526,141 @@ def w4a8_stream_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos
 
 def w4a8_stream_attention_workspace_bytes(H: int, Nq: int, Nk: int) -> int:
     return int(lib().w4a8_stream_attention_workspace_bytes(H, Nq, Nk))
+
+
+class KVCache(NamedTuple):
+    """The tensors of an 8-bit key/value cache, a pool of pages of CACHE_BLOCK
+    tokens: codes of the keys int8 [pages][Hkv][64][128] and of the values
+    int8 [pages][Hkv][128][64] (d by token), scales fp32 [pages][Hkv][2]
+    (keys', values'), and the rings of exact values that the append needs,
+    bf16 [slots][Hkv][128][128] (None where the cache is only read).
+
+    The values that a page stands for: k_codes[p] * scales[p, :, 0, None, None]
+    and v_codes[p] * scales[p, :, 1, None, None]."""
+
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    scales: torch.Tensor
+    k_recent: torch.Tensor | None = None
+    v_recent: torch.Tensor | None = None
+
+    @classmethod
+    def empty(cls, pages: int, slots: int, Hkv: int, device="cuda") -> "KVCache":
+        """A zero-filled cache of `pages` pages and rings for `slots` sequences."""
+        z = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
+        ring = (slots, Hkv, CACHE_RECENT, HEAD_DIM)
+        return cls(z(pages, Hkv, CACHE_BLOCK, HEAD_DIM, dtype=torch.int8), z(pages, Hkv, HEAD_DIM, CACHE_BLOCK, dtype=torch.int8),
+                   z(pages, Hkv, 2, dtype=torch.float32), z(*ring, dtype=torch.bfloat16), z(*ring, dtype=torch.bfloat16))
+
+
+def _cache_args(cache: KVCache, rings: bool) -> tuple[_CacheArgs, int]:
+    """The library's view of a cache, its shapes checked, and its kv heads."""
+    k = cache.k_codes
+    if k.dim() != 4 or tuple(k.shape[2:]) != (CACHE_BLOCK, HEAD_DIM):
+        raise ValueError(f"k_codes must be [pages][Hkv][{CACHE_BLOCK}][{HEAD_DIM}]")
+    pages, Hkv = k.shape[:2]
+    if tuple(cache.v_codes.shape) != (pages, Hkv, HEAD_DIM, CACHE_BLOCK):
+        raise ValueError(f"v_codes must be [{pages}][{Hkv}][{HEAD_DIM}][{CACHE_BLOCK}]")
+    if tuple(cache.scales.shape) != (pages, Hkv, 2):
+        raise ValueError(f"scales must be [{pages}][{Hkv}][2]")
+    a = _CacheArgs(_dev(k, "k_codes", torch.int8), _dev(cache.v_codes, "v_codes", torch.int8),
+                   _dev(cache.scales, "scales", torch.float32), pages, Hkv, None, None, 0)
+    if rings:
+        if cache.k_recent is None or cache.v_recent is None:
+            raise ValueError("the append needs the cache's k_recent and v_recent")
+        a.n_slots = cache.k_recent.shape[0]
+        for name, t in (("k_recent", cache.k_recent), ("v_recent", cache.v_recent)):
+            if tuple(t.shape) != (a.n_slots, Hkv, CACHE_RECENT, HEAD_DIM):
+                raise ValueError(f"{name} must be [slots][{Hkv}][{CACHE_RECENT}][{HEAD_DIM}], with the slots of k_recent")
+        a.k_recent = _dev(cache.k_recent, "k_recent", torch.bfloat16)
+        a.v_recent = _dev(cache.v_recent, "v_recent", torch.bfloat16)
+    return a, Hkv
+
+
+def _batch_args(T, starts, lengths, table, pos, rope_cos, rope_sin) -> _BatchArgs:
+    """The library's view of a batch of T new tokens, its shapes checked."""
+    B = lengths.shape[0]
+    if lengths.dim() != 1 or tuple(starts.shape) != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("starts, lengths and table must be [B + 1], [B] and [B][blocks]")
+    if tuple(pos.shape) != (T,):
+        raise ValueError(f"pos must be [{T}]")
+    if rope_cos.shape != rope_sin.shape or rope_cos.dim() != 2 or rope_cos.shape[1] != HEAD_DIM // 2:
+        raise ValueError(f"rotary tables must be [n_pos][{HEAD_DIM // 2}]")
+    i32 = torch.int32
+    return _BatchArgs(_dev(starts, "starts", i32), _dev(lengths, "lengths", i32), _dev(table, "table", i32), table.shape[1],
+                      B, T, _dev(pos, "pos", i32), _dev(rope_cos, "rope_cos", torch.float32),
+                      _dev(rope_sin, "rope_sin", torch.float32), rope_cos.shape[0])
+
+
+def _token_rows(t: torch.Tensor, name: str):
+    """(pointer, token stride, head stride) of bf16 [T][heads][128], whose last
+    axis alone has to be contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[2] != HEAD_DIM:
+        raise ValueError(f"{name} must be [T][heads][{HEAD_DIM}]")
+    if t.numel() and t.stride(2) != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    row, head = (HEAD_DIM if t.shape[i] <= 1 else t.stride(i) for i in (0, 1))  # the stride of an axis of one is free
+    return t.data_ptr(), row, head
+
+
+def w4a8_cache_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, starts: torch.Tensor, lengths: torch.Tensor,
+                      table: torch.Tensor, pos: torch.Tensor, rope_cos: torch.Tensor, rope_sin: torch.Tensor,
+                      slots: torch.Tensor | None = None, stream=None) -> None:
+    """Append a step's new keys (rotated at `pos`) and values to the 8-bit
+    cache, in place.  k, v: bf16 [T][Hkv][128], strided views allowed.  The
+    batch: int32 starts [B + 1] (rows starts[b] .. are sequence b's new
+    tokens), lengths [B] (tokens held, the new ones included), table
+    [B][blocks] (pages), pos [T]; fp32 rotary tables [n_pos][64]; slots int32
+    [B], the ring of each sequence (None: sequence b has ring b)."""
+    T = k.shape[0]
+    k_rows, v_rows = _token_rows(k, "k"), _token_rows(v, "v")
+    c, Hkv = _cache_args(cache, True)
+    if k.shape[1] != Hkv or v.shape != k.shape:
+        raise ValueError(f"k and v must be [T][{Hkv}][{HEAD_DIM}]")
+    b = _batch_args(T, starts, lengths, table, pos, rope_cos, rope_sin)
+    if slots is not None and tuple(slots.shape) != (b.B,):
+        raise ValueError(f"slots must be [{b.B}]")
+    sl = None if slots is None else _dev(slots, "slots", torch.int32)
+    with _call_on(stream, k, v=v, starts=starts, lengths=lengths, table=table, pos=pos, rope_cos=rope_cos, rope_sin=rope_sin,
+                  slots=slots, **cache._asdict()) as s:
+        rc = lib().w4a8_cache_append(c, b, *k_rows, *v_rows, sl, s.cuda_stream)
+    _check(rc, "w4a8_cache_append")
+
+
+def w4a8_cache_attention_workspace_bytes(B: int, T: int, H: int, Hkv: int, max_len: int) -> int:
+    return int(lib().w4a8_cache_attention_workspace_bytes(B, T, H, Hkv, max_len))
+
+
+def w4a8_cache_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
+                         pos: torch.Tensor, rope_cos: torch.Tensor, rope_sin: torch.Tensor, scale: float,
+                         max_len: int | None = None, out: torch.Tensor | None = None,
+                         workspace: Workspace | torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of a step's new tokens over the 8-bit cache that holds them
+    already (w4a8_cache_append): q bf16 [T][H][128], strided views allowed ->
+    bf16 [T][H][128] (`out` may be a strided view too; rows of no sequence
+    are not written).  New token i of n of a sequence of length L sees its
+    tokens up to L - n + i.  The batch is that of w4a8_cache_append; max_len,
+    an upper bound of the lengths (the table's by default), only decides how
+    the work is split."""
+    T, H = q.shape[0], q.shape[1]
+    q_rows = _token_rows(q, "q")
+    c, Hkv = _cache_args(cache, False)
+    b = _batch_args(T, starts, lengths, table, pos, rope_cos, rope_sin)
+    if max_len is None:
+        max_len = b.max_blocks * CACHE_BLOCK
+    if out is not None and out.shape != q.shape:
+        raise ValueError(f"out must be [{T}][{H}][{HEAD_DIM}]")
+    with _call_on(stream, q, k_codes=cache.k_codes, v_codes=cache.v_codes, scales=cache.scales, starts=starts, lengths=lengths,
+                  table=table, pos=pos, rope_cos=rope_cos, rope_sin=rope_sin, out=out) as s:
+        if out is None:
+            out = torch.empty((T, H, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
+        need = w4a8_cache_attention_workspace_bytes(b.B, T, H, Hkv, max_len)
+        wk_ptr, wk_bytes = _workspace_ptr(workspace, need, q.device, s)
+        rc = lib().w4a8_cache_attention(c, b, *q_rows, H, float(scale), max_len, *_token_rows(out, "out"), wk_ptr, wk_bytes,
+                                        s.cuda_stream)
+    _check(rc, "w4a8_cache_attention")
+    return out

@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "attention.h"
+#include "cache.h"
 #include "kernels.h"
 
 using namespace w4a8;
@@ -19,6 +20,11 @@ constexpr int64_t kNMax = int64_t(1) << 24;
 static_assert(W4A8_NOALLOC_SCRATCH_BYTES == kNoAllocScratchBytes, "header and library agree on the scratch size");
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+// whether [a, a + na) and [b, b + nb) share a byte
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 bool valid_nk(int64_t N, int64_t K) {
@@ -196,6 +202,53 @@ const char* describe(int64_t M, int64_t N, int64_t K, int scale_mode, int in_kin
   return buf;
 }
 
+// ---- the 8-bit cache
+
+constexpr int64_t kCacheHeadsMax = 4096, kCacheBatchMax = 65536, kI32Max = 0x7FFFFFFF;
+
+// Sizes and pointers that the append and the attention have in common.
+w4a8_status check_cache(const w4a8_cache* c, const w4a8_batch* b, CacheBatch* out) {
+  if (!c || !b) return W4A8_EINVAL;
+  if (c->Hkv < 1 || c->Hkv > kCacheHeadsMax || c->n_pages < 1 || c->n_pages > kI32Max) return W4A8_EINVAL;
+  if (b->B < 0 || b->B > kCacheBatchMax || b->T < 0 || b->T > W4A8_M_MAX) return W4A8_EINVAL;
+  if (b->max_blocks < 1 || b->max_blocks > (int64_t(1) << 24) || b->n_pos < 1 || b->n_pos > (int64_t(1) << 30))
+    return W4A8_EINVAL;
+  if (b->B == 0 || b->T == 0) return W4A8_OK;
+  if (!c->k_codes || !c->v_codes || !c->scales || !aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) ||
+      !aligned(c->scales, 8))
+    return W4A8_EINVAL;
+  if (!b->starts || !b->lengths || !b->table || !b->pos || !b->rope_cos || !b->rope_sin || !aligned(b->starts, 4) ||
+      !aligned(b->lengths, 4) || !aligned(b->table, 4) || !aligned(b->pos, 4) || !aligned(b->rope_cos, 16) ||
+      !aligned(b->rope_sin, 16))
+    return W4A8_EINVAL;
+  out->k_codes = c->k_codes;
+  out->v_codes = c->v_codes;
+  out->scales = c->scales;
+  out->n_pages = c->n_pages;
+  out->starts = b->starts;
+  out->lengths = b->lengths;
+  out->table = b->table;
+  out->max_blocks = (int)b->max_blocks;
+  out->B = (int)b->B;
+  out->T = (int)b->T;
+  out->Hkv = (int)c->Hkv;
+  out->pos = b->pos;
+  out->rope_cos = b->rope_cos;
+  out->rope_sin = b->rope_sin;
+  out->n_pos = (int)b->n_pos;
+  return W4A8_OK;
+}
+
+bool valid_rows(const uint16_t* p, int64_t row, int64_t head) {
+  constexpr int64_t kMax = int64_t(1) << 40;
+  return p && aligned(p, 16) && row >= 0 && head >= 0 && row <= kMax && head <= kMax && row % 8 == 0 && head % 8 == 0;
+}
+
+bool valid_cache_attention(int64_t B, int64_t T, int64_t H, int64_t Hkv, int64_t max_len) {
+  return B >= 0 && B <= kCacheBatchMax && T >= 0 && T <= W4A8_M_MAX && Hkv >= 1 && H >= 1 && H <= kCacheHeadsMax &&
+         H % Hkv == 0 && max_len >= 1 && max_len <= (int64_t(1) << 30);
+}
+
 }  // namespace
 
 extern "C" {
@@ -251,6 +304,30 @@ w4a8_status w4a8_rmsnorm_quantize_act(const uint16_t* x, const uint16_t* gamma, 
     return W4A8_EINVAL;
   return launch_rmsnorm_quantize(x, gamma, eps, (int)M, (int)K, x_q, x_scale, stream) == hipSuccess ? W4A8_OK
                                                                                                   : W4A8_EHIP;
+}
+
+w4a8_status w4a8_add_rmsnorm_quantize_act(const uint16_t* x, const uint16_t* residual, const uint16_t* gamma, float eps,
+                                          int64_t M, int64_t K, uint16_t* sum, int8_t* x_q, float* x_scale,
+                                          hipStream_t stream) {
+  if (M < 0 || M > W4A8_M_MAX) return W4A8_EINVAL;
+  if (K < W4A8_GROUP_SIZE || K % W4A8_GROUP_SIZE || K > W4A8_K_MAX) return W4A8_EINVAL;
+  if (!(eps > 0.0f) || !(eps <= 3.4e38f)) return W4A8_EINVAL;  // also rejects NaN and inf
+  if (M == 0) return W4A8_OK;
+  if (!x || !residual || !gamma || !sum || !x_q || !x_scale || !aligned(x, 16) || !aligned(residual, 16) ||
+      !aligned(gamma, 16) || !aligned(sum, 16) || !aligned(x_q, 16) || !aligned(x_scale, 4))
+    return W4A8_EINVAL;
+  // What a workgroup writes no other may read: the sum lies on x or residual exactly, or apart.
+  const size_t rows = (size_t)M * K * 2, out[3] = {rows, rows / 2, (size_t)M * 4}, in[3] = {rows, rows, (size_t)K * 2};
+  const void *o[3] = {sum, x_q, x_scale}, *i[3] = {x, residual, gamma};
+  for (int a = 0; a < 3; ++a) {
+    for (int b = 0; b < 3; ++b)
+      if (overlap(o[a], out[a], i[b], in[b]) && !(a == 0 && b < 2 && o[0] == i[b])) return W4A8_EINVAL;
+    for (int b = 0; b < a; ++b)
+      if (overlap(o[a], out[a], o[b], out[b])) return W4A8_EINVAL;
+  }
+  return launch_add_rmsnorm_quantize(x, residual, gamma, eps, (int)M, (int)K, sum, x_q, x_scale, stream) == hipSuccess
+             ? W4A8_OK
+             : W4A8_EHIP;
 }
 
 w4a8_status w4a8_flow_schedule(int64_t n_steps, int64_t n_reuse, int32_t* fresh) {
@@ -330,6 +407,61 @@ w4a8_status w4a8_stream_attention(const uint16_t* q, const uint16_t* k, const ui
   a.scale_log2e = (scale == 0.0f ? 1.0f : std::fabs(scale)) * 1.4426950408889634f;
   a.q_sign = scale == 0.0f ? 0.0f : scale < 0.0f ? -1.0f : 1.0f;
   return launch_stream_attention(a, stream) == hipSuccess ? W4A8_OK : W4A8_EHIP;
+}
+
+w4a8_status w4a8_cache_append(const w4a8_cache* cache, const w4a8_batch* batch, const uint16_t* k, int64_t k_row,
+                              int64_t k_head, const uint16_t* v, int64_t v_row, int64_t v_head, const int32_t* slots,
+                              hipStream_t stream) {
+  CacheAppendArgs a{};
+  const w4a8_status s = check_cache(cache, batch, &a.c);
+  if (s != W4A8_OK) return s;
+  if (cache->n_slots < 1 || cache->n_slots > kI32Max) return W4A8_EINVAL;
+  if (batch->B == 0 || batch->T == 0) return W4A8_OK;
+  if (!cache->k_recent || !cache->v_recent || !aligned(cache->k_recent, 16) || !aligned(cache->v_recent, 16))
+    return W4A8_EINVAL;
+  if (!valid_rows(k, k_row, k_head) || !valid_rows(v, v_row, v_head) || !aligned(slots, 4)) return W4A8_EINVAL;
+  a.k = {const_cast<uint16_t*>(k), k_row, k_head};
+  a.v = {const_cast<uint16_t*>(v), v_row, v_head};
+  a.k_recent = cache->k_recent;
+  a.v_recent = cache->v_recent;
+  a.n_slots = cache->n_slots;
+  a.slots = slots;
+  return launch_cache_append(a, stream) == hipSuccess ? W4A8_OK : W4A8_EHIP;
+}
+
+size_t w4a8_cache_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hkv, int64_t max_len) {
+  if (!valid_cache_attention(B, T, H, Hkv, max_len) || B == 0 || T == 0) return 0;
+  return cache_attention_workspace((int)B, (int)T, (int)H, (int)Hkv, (int)max_len);
+}
+
+w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batch, const uint16_t* q, int64_t q_row,
+                                 int64_t q_head, int64_t H, float scale, int64_t max_len, uint16_t* o, int64_t o_row,
+                                 int64_t o_head, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  CacheAttnArgs a{};
+  const w4a8_status s = check_cache(cache, batch, &a.c);
+  if (s != W4A8_OK) return s;
+  if (!valid_cache_attention(batch->B, batch->T, H, cache->Hkv, max_len) ||
+      max_len > batch->max_blocks * W4A8_CACHE_BLOCK)
+    return W4A8_EINVAL;
+  if (!(scale == scale) || scale > 3.4e38f || scale < -3.4e38f) return W4A8_EINVAL;  // finite
+  if (batch->B == 0 || batch->T == 0) return W4A8_OK;
+  if (!valid_rows(q, q_row, q_head) || !valid_rows(o, o_row, o_head)) return W4A8_EINVAL;
+  // output rows apart: heads within tokens, or tokens within heads
+  const int64_t T = batch->T, D = kCacheD;
+  if (!(((H == 1 || o_head >= D) && (T == 1 || o_row >= (H - 1) * o_head + D)) ||
+        ((T == 1 || o_row >= D) && (H == 1 || o_head >= (T - 1) * o_row + D))))
+    return W4A8_EINVAL;
+  const size_t need = cache_attention_workspace(a.c.B, a.c.T, (int)H, a.c.Hkv, (int)max_len);
+  if (need && (workspace_bytes < need || !workspace || !aligned(workspace, 256))) return W4A8_EINVAL;
+  a.q = {const_cast<uint16_t*>(q), q_row, q_head};
+  a.o = {o, o_row, o_head};
+  a.H = (int)H;
+  // as in w4a8_stream_attention, the queries carry the scale's sign, or its zero
+  a.scale_log2e = (scale == 0.0f ? 1.0f : std::fabs(scale)) * 1.4426950408889634f;
+  a.q_sign = scale == 0.0f ? 0.0f : scale < 0.0f ? -1.0f : 1.0f;
+  a.max_len = (int)max_len;
+  a.workspace = workspace;
+  return launch_cache_attention(a, stream) == hipSuccess ? W4A8_OK : W4A8_EHIP;
 }
 
 size_t w4a8_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int scale_mode, int in_kind) {

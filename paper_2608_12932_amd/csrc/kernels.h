@@ -22,6 +22,9 @@ hipError_t launch_quantize(const uint16_t* x, int M, int K, int8_t* q, float* sc
 // RMSNorm (gain gamma, eps > 0) of each row, then the quantize of the fp32 result
 hipError_t launch_rmsnorm_quantize(const uint16_t* x, const uint16_t* gamma, float eps, int M, int K, int8_t* q,
                                    float* scale, hipStream_t stream);
+// the same of each row's sum bf16(x + residual), which is stored to `sum` (x or residual itself, or apart)
+hipError_t launch_add_rmsnorm_quantize(const uint16_t* x, const uint16_t* residual, const uint16_t* gamma, float eps,
+                                       int M, int K, uint16_t* sum, int8_t* q, float* scale, hipStream_t stream);
 
 // ---- weight pack (pack.hip); `err` is a device word set to 1 on a range error
 hipError_t launch_pack(const int8_t* w, int N, int K, uint8_t* out, unsigned* err,

@@ -112,27 +112,54 @@ __global__ __launch_bounds__(kWaveThreads) void quantize_rows_wave(const uint16_
 // one chain of latencies, so every thread folds the waves' results and forms
 // r and the scale itself (one barrier each), and the waves reduce without
 // LDS; with many the divisions were a third of the vector work.
-template <int T, int C>
-__global__ __launch_bounds__(T) void rmsnorm_quantize_rows(const uint16_t* __restrict__ x,
+//
+// ADD: the row is the residual stream's sum bf16(x + residual), one fp32
+// addition and one rounding, stored to `sum` and normalized as it is stored,
+// so that codes and scales are those of a separate addition in front.  `sum`
+// may be `x` or `residual` itself: a thread stores a chunk after it has read
+// both inputs there, and reads a stored chunk back only where it stored it
+// (the chunks past C T), so neither pointer is restrict.
+template <int T, int C, bool ADD>
+__global__ __launch_bounds__(T) void rmsnorm_quantize_rows(const uint16_t* x, const uint16_t* residual,
                                                            const uint16_t* __restrict__ gamma, float eps, int K,
-                                                           int8_t* __restrict__ q, float* __restrict__ scale) {
+                                                           uint16_t* sum, int8_t* __restrict__ q,
+                                                           float* __restrict__ scale) {
   const int row = blockIdx.x;
   const int tid = threadIdx.x;
-  const uint4* xr = reinterpret_cast<const uint4*>(x + (size_t)row * K);
+  // the row that is normalized: x, or with ADD the stored sum
+  const uint4* xr = reinterpret_cast<const uint4*>((ADD ? sum : x) + (size_t)row * K);
   const uint4* gr = reinterpret_cast<const uint4*>(gamma);
   uint2* qr = reinterpret_cast<uint2*>(q + (size_t)row * K);
   const int nchunk = K / 8;
-  const __amdgpu_buffer_rsrc_t xres = make_rsrc(xr, (uint32_t)(K * 2));
+  const __amdgpu_buffer_rsrc_t xres = make_rsrc(x + (size_t)row * K, (uint32_t)(K * 2));
   const __amdgpu_buffer_rsrc_t gres = make_rsrc(gr, (uint32_t)(K * 2));
-  uint4 xc[C], gc[C];
+  const __amdgpu_buffer_rsrc_t rres = make_rsrc(ADD ? residual + (size_t)row * K : x, (uint32_t)(K * 2));
+  uint4 xc[C], gc[C], rc[C];
 #pragma unroll
   for (int j = 0; j < C; ++j) {
     const int c = tid + j * T;
     const uint32_t off = c < nchunk ? (uint32_t)(c * 16) : kOOB;
     xc[j] = buf_load16(xres, off);
+    if constexpr (ADD) rc[j] = buf_load16(rres, off);
     gc[j] = buf_load16(gres, off);
   }
   auto words = [](const uint4& v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; };
+  if constexpr (ADD) {
+    auto add = [](uint32_t a, uint32_t b) { return bf16x2_bits(bf16_lo(a) + bf16_lo(b), bf16_hi(a) + bf16_hi(b)); };
+    auto add_chunk = [&](const uint4& a, const uint4& b) {
+      return make_uint4(add(a.x, b.x), add(a.y, b.y), add(a.z, b.z), add(a.w, b.w));
+    };
+    uint4* sr = reinterpret_cast<uint4*>(sum + (size_t)row * K);
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int c = tid + j * T;
+      xc[j] = add_chunk(xc[j], rc[j]);
+      if (c < nchunk) sr[c] = xc[j];
+    }
+    const uint4 *x0 = reinterpret_cast<const uint4*>(x + (size_t)row * K),
+                *r0 = reinterpret_cast<const uint4*>(residual + (size_t)row * K);
+    for (int c = tid + C * T; c < nchunk; c += T) sr[c] = add_chunk(x0[c], r0[c]);
+  }
   auto sq_sum = [&](const uint4& v, double acc) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -228,15 +255,15 @@ __global__ __launch_bounds__(T) void rmsnorm_quantize_rows(const uint16_t* __res
   for (int c = tid + C * T; c < nchunk; c += T) qr[c] = codes(xr[c], gr[c]);
 }
 
-typedef void (*NormQuantFn)(const uint16_t*, const uint16_t*, float, int, int8_t*, float*);
+typedef void (*NormQuantFn)(const uint16_t*, const uint16_t*, const uint16_t*, float, int, uint16_t*, int8_t*, float*);
 
-template <int T>
+template <int T, bool ADD>
 NormQuantFn norm_kernel(int C) {
   switch (C) {
-    case 1: return rmsnorm_quantize_rows<T, 1>;
-    case 2: return rmsnorm_quantize_rows<T, 2>;
-    case 4: return rmsnorm_quantize_rows<T, 4>;
-    default: return rmsnorm_quantize_rows<T, 8>;
+    case 1: return rmsnorm_quantize_rows<T, 1, ADD>;
+    case 2: return rmsnorm_quantize_rows<T, 2, ADD>;
+    case 4: return rmsnorm_quantize_rows<T, 4, ADD>;
+    default: return rmsnorm_quantize_rows<T, 8, ADD>;
   }
 }
 
@@ -288,8 +315,11 @@ hipError_t launch_quantize(const uint16_t* x, int M, int K, int8_t* q, float* sc
   return hipGetLastError();
 }
 
-hipError_t launch_rmsnorm_quantize(const uint16_t* x, const uint16_t* gamma, float eps, int M, int K, int8_t* q,
-                                   float* scale, hipStream_t stream) {
+namespace {
+
+template <bool ADD>
+hipError_t launch_norm(const uint16_t* x, const uint16_t* residual, const uint16_t* gamma, float eps, int M, int K,
+                       uint16_t* sum, int8_t* q, float* scale, hipStream_t stream) {
   if (M == 0) return hipSuccess;
   // the quantize launcher's shapes, one workgroup of at least 128 threads per row
   const int nchunk = K / 8;
@@ -298,9 +328,22 @@ hipError_t launch_rmsnorm_quantize(const uint16_t* x, const uint16_t* gamma, flo
   while (T < 512 && T * per < nchunk) T *= 2;
   int C = 1;
   while (C < 8 && C * T < nchunk) C *= 2;
-  const NormQuantFn k = T == 128 ? norm_kernel<128>(C) : T == 256 ? norm_kernel<256>(C) : norm_kernel<512>(C);
-  k<<<dim3(M), dim3(T), 0, stream>>>(x, gamma, eps, K, q, scale);
+  const NormQuantFn k =
+      T == 128 ? norm_kernel<128, ADD>(C) : T == 256 ? norm_kernel<256, ADD>(C) : norm_kernel<512, ADD>(C);
+  k<<<dim3(M), dim3(T), 0, stream>>>(x, residual, gamma, eps, K, sum, q, scale);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm_quantize(const uint16_t* x, const uint16_t* gamma, float eps, int M, int K, int8_t* q,
+                                   float* scale, hipStream_t stream) {
+  return launch_norm<false>(x, nullptr, gamma, eps, M, K, nullptr, q, scale, stream);
+}
+
+hipError_t launch_add_rmsnorm_quantize(const uint16_t* x, const uint16_t* residual, const uint16_t* gamma, float eps,
+                                       int M, int K, uint16_t* sum, int8_t* q, float* scale, hipStream_t stream) {
+  return launch_norm<true>(x, residual, gamma, eps, M, K, sum, q, scale, stream);
 }
 
 }  // namespace w4a8
