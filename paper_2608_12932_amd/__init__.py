@@ -246,6 +246,10 @@ def w4a8_add_rmsnorm_quantize_act(x: torch.Tensor, residual: torch.Tensor, gamma
     sum = bf16(x + residual) for bf16 x, residual [M][K] -> (codes int8
     [M][K], scales fp32 [M], sum bf16 [M][K]).  `out` takes the sum and may be
     x or residual itself."""
+    if stream is None:
+        r = (_fast or _load_fast()).add_norm(x, residual, gamma, eps, out)
+        if r is not None:
+            return r if type(r) is tuple else _check(r, "w4a8_add_rmsnorm_quantize_act")
     M, K = x.shape
     x_ptr, r_ptr = _dev(x, "x", torch.bfloat16), _dev(residual, "residual", torch.bfloat16)
     g_ptr = _dev(gamma, "gamma", torch.bfloat16)
@@ -367,16 +371,20 @@ def _workspace_ptr(workspace, need: int, device, stream):
     return _dev(buf, "workspace", torch.uint8), buf.numel()
 
 
+def _workspace_of(workspace):
+    """(buffer, the stream that its memory is ordered on, whether it is a
+    Workspace's) for the native path."""
+    if type(workspace) is Workspace:
+        buf, home = workspace._home
+        return (buf, home, True) if buf is workspace.buf else (None, None, True)
+    return workspace, None, False
+
+
 def _linear_fast(swiglu: int, x, w_packed, w_scale, N, x_scale, scale_mode, out_kind, out, workspace):
     """The native path of both linear calls on the current stream; None where
     it does not take the call (a Workspace that belongs to another stream,
     arguments that need an error, ...)."""
-    buf, home, own = workspace, None, False
-    if type(workspace) is Workspace:
-        own = True
-        buf, home = workspace._home
-        if buf is not workspace.buf:
-            buf = home = None
+    buf, home, own = _workspace_of(workspace)
     fast = _fast or _load_fast()
     r = fast.linear(swiglu, x, w_packed, w_scale, N, x_scale, scale_mode, out_kind, out, buf, home, own)
     if type(r) is int:
@@ -616,6 +624,10 @@ def w4a8_cache_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, starts: 
     tokens), lengths [B] (tokens held, the new ones included), table
     [B][blocks] (pages), pos [T]; fp32 rotary tables [n_pos][64]; slots int32
     [B], the ring of each sequence (None: sequence b has ring b)."""
+    if stream is None:
+        r = (_fast or _load_fast()).cache_append(k, v, cache, starts, lengths, table, pos, rope_cos, rope_sin, slots)
+        if r is not None:
+            return None if r is True else _check(r, "w4a8_cache_append")
     T = k.shape[0]
     k_rows, v_rows = _token_rows(k, "k"), _token_rows(v, "v")
     c, Hkv = _cache_args(cache, True)
@@ -646,6 +658,15 @@ def w4a8_cache_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, 
     tokens up to L - n + i.  The batch is that of w4a8_cache_append; max_len,
     an upper bound of the lengths (the table's by default), only decides how
     the work is split."""
+    if stream is None:
+        buf, home, own = _workspace_of(workspace)
+        r = (_fast or _load_fast()).cache_attention(q, cache, starts, lengths, table, pos, rope_cos, rope_sin, scale, max_len, out, buf,
+                                                    home, own)
+        if type(r) is int and r < 0:  # the bytes that the Workspace, on this stream or still empty, lacks
+            workspace.get(-r)
+            return w4a8_cache_attention(q, cache, starts, lengths, table, pos, rope_cos, rope_sin, scale, max_len, out, workspace)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "w4a8_cache_attention")
     T, H = q.shape[0], q.shape[1]
     q_rows = _token_rows(q, "q")
     c, Hkv = _cache_args(cache, False)

@@ -42,6 +42,23 @@ __device__ __forceinline__ void sequence(const CacheBatch& c, int b, int& row0, 
   len = min(max(c.lengths[b], 0), c.max_blocks * kBlock);
 }
 
+// Inclusive sum over the wave's lanes, by lane moves in the vector unit: within
+// rows of 16, then each row's total into the rows after it.
+__device__ __forceinline__ int wave_scan(int v) {
+  constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+  auto step = [&](auto ctrl, auto rows) {  // lanes without a source add 0
+    v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+  };
+  using std::integral_constant;
+  step(integral_constant<int, kRowShr + 1>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, kRowShr + 2>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, kRowShr + 4>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, kRowShr + 8>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, kRowBcast15>{}, integral_constant<int, 0xA>{});
+  step(integral_constant<int, kRowBcast31>{}, integral_constant<int, 0xC>{});
+  return v;
+}
+
 // The sequence that work item `item` belongs to, when sequence b has
 // count(n, len) items and they are numbered through the batch.  Every wave
 // finds it by itself, 64 sequences at a time.
@@ -56,12 +73,7 @@ __device__ __forceinline__ Sequence find_sequence(const CacheBatch& c, int item,
       sequence(c, b, row0, n, len);
       cnt = count(n, len);
     }
-    int upto = cnt;  // inclusive scan
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int u = __shfl_up(upto, off, 64);
-      if (lane >= off) upto += u;
-    }
+    const int upto = wave_scan(cnt);
     const uint64_t past = __ballot(base + upto > item);
     if (past) {
       const int l = __builtin_ctzll(past);
@@ -284,9 +296,9 @@ __device__ __forceinline__ float fold_groups(float x, F op) {
 
 // One workgroup per (rows of one sequence's kv head, split of its blocks).
 // A row is a (new token, query head of the kv head) pair, row i G + g; a wave
-// holds R tiles of 16 rows.  SHARED: the four waves hold the same rows and
-// take every fourth block each, meeting in LDS at the end; otherwise each
-// holds rows of its own and goes through all blocks.
+// holds R tiles of 16 rows.  KW waves hold the same rows and take every KW-th
+// block each, meeting in LDS at the end; the 4 / KW groups of waves hold
+// different rows.
 //
 // Per block of 64 tokens, with everything in registers (the page's layout is
 // the operands'):
@@ -299,13 +311,12 @@ __device__ __forceinline__ float fold_groups(float x, F op) {
 //     with the values' codes in fp16 (exact) for O^T += V^T P^T: the values'
 //     scale is inside the weight, and comes out of the weights' total through
 //     its reciprocal.
-template <int R, bool SHARED>
+template <int R, int KW>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const CacheAttnArgs a) {
-  constexpr int kWaveRows = 16 * R, kRows = SHARED ? kWaveRows : kAttnWaves * kWaveRows;
-  constexpr int kStep = SHARED ? kAttnWaves : 1;
+  constexpr int kWaveRows = 16 * R, kRows = kAttnWaves / KW * kWaveRows;
   constexpr int kPitch = kD + 4;  // floats of a row in the merge
-  __shared__ __align__(16) float l_o[SHARED ? kAttnWaves * kWaveRows * kPitch : 4];
-  __shared__ float2 l_ml[SHARED ? kAttnWaves * kWaveRows : 1];
+  __shared__ __align__(16) float l_o[KW > 1 ? kAttnWaves * kWaveRows * kPitch : 4];
+  __shared__ float2 l_ml[KW > 1 ? kAttnWaves * kWaveRows : 1];
 
   const CacheBatch& cb = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -315,7 +326,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
   const Sequence s =
       find_sequence(cb, rest / a.S, [&](int n, int) { return (int)(((int64_t)n * G + kRows - 1) / kRows); });
   if (s.b < 0) return;
-  const int n_rows = s.n * G, row0 = s.item * kRows + (SHARED ? 0 : wave * kWaveRows);
+  const int kw = wave % KW, n_rows = s.n * G, row0 = s.item * kRows + wave / KW * kWaveRows;
   // tokens that the workgroup's (the wave's) last row sees
   auto seen_by = [&](int row) { return s.len - s.n + min(row, n_rows - 1) / G + 1; };
   const int blocks_wg = (max(seen_by(s.item * kRows + kRows - 1), 0) + kBlock - 1) / kBlock;
@@ -323,43 +334,87 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
   const int seen = row0 < n_rows ? max(seen_by(row0 + kWaveRows - 1), 0) : 0;
   const int p_begin = split * per, p_end = min(p_begin + per, (seen + kBlock - 1) / kBlock);
 
-  // ---- this lane's rows (row l16 of each tile): the rotated query's digits
-  // for d = 16 g .. and 64 + 16 g .., the B operand of the int8 MFMAs
-  v4i qh[R][2], ql[R][2];
-  float row_scale[R];  // of a score, in base-2 units, before the block's
-  int last_key[R];     // the last token that the row sees, -1 for a row past the end
+  // ---- the wave's blocks p = p_first + KW i, i < count; lane j of the
+  // registers below holds what block 64 (i / 64) + j needs
+  const int p_first = p_begin + kw;
+  const int count = p_end > p_first ? (p_end - p_first + KW - 1) / KW : 0;
+  int page_l = -1;
+  float2 scales_l;
+  auto fetch_pages = [&](int i0) {
+    const int i = i0 + lane;
+    page_l = i < count ? cb.table[(int64_t)s.b * cb.max_blocks + p_first + KW * i] : -1;
+    if (page_l >= cb.n_pages) page_l = -1;  // no page (as below 0): tokens that no row sees
+  };
+  auto fetch_scales = [&] {
+    scales_l = make_float2(0.0f, 0.0f);
+    if (page_l >= 0) scales_l = *reinterpret_cast<const float2*>(cb.scales + ((int64_t)page_l * cb.Hkv + hk) * 2);
+  };
+  auto resource = [&](const int8_t* codes, int page) {  // an empty one where there is no page
+    return make_rsrc(codes + ((int64_t)max(page, 0) * cb.Hkv + hk) * kPageBytes, page < 0 ? 0u : (uint32_t)kPageBytes);
+  };
+  // K: row m of tile t is token 16 (m / 4) + 4 t + m % 4, so that lane group g
+  // gets the scores of tokens 16 g + 4 t ..; V: row d, tokens 16 g ..
+  const uint32_t k_off = (uint32_t)((16 * (l16 >> 2) + (l16 & 3)) * kD + 16 * g);
+  const uint32_t v_off = (uint32_t)(l16 * kBlock + 16 * g);
+  uint4 kr[4][2], vr[8];
+  auto load_keys = [&](int page) {
+    const __amdgpu_buffer_rsrc_t r = resource(cb.k_codes, page);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) kr[t][h] = buf_load16(r, k_off + (uint32_t)(4 * t * kD + 64 * h));
+  };
+  auto load_values = [&](int page) {
+    const __amdgpu_buffer_rsrc_t r = resource(cb.v_codes, page);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) vr[d] = buf_load16(r, v_off + (uint32_t)(16 * d * kBlock));
+  };
+  fetch_pages(0);
+
+  // ---- this lane's rows (row l16 of each tile): the query's d = 16 g .. and
+  // 64 + 16 g .. and the table row, requested before the first block's codes
+  uint4 qr[R][4];
+  float4 cs4[R][4], sn4[R][4];
+  int last_key[R];  // the last token that the row sees, -1 for a row past the end
 #pragma unroll
   for (int t = 0; t < R; ++t) {
     const int row = row0 + 16 * t + l16;
     const bool ok = row < n_rows;
-    const int i = ok ? row / G : 0, tok = s.row0 + i;
+    const int i = ok ? row / G : 0, tok = s.row0 + i;  // a row past the end reads the sequence's first
     last_key[t] = ok ? s.len - s.n + i : -1;
+    const uint16_t* src = a.q.p + tok * a.q.row + (hk * G + (ok ? row - i * G : 0)) * a.q.head + 16 * g;
+    const int64_t at = (int64_t)clamp_pos(cb.pos[tok], cb.n_pos) * kHalf + 16 * g;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      qr[t][e] = *reinterpret_cast<const uint4*>(src + (e >> 1) * kHalf + (e & 1) * 8);
+      cs4[t][e] = *reinterpret_cast<const float4*>(cb.rope_cos + at + 4 * e);
+      sn4[t][e] = *reinterpret_cast<const float4*>(cb.rope_sin + at + 4 * e);
+    }
+  }
+  int page = __builtin_amdgcn_readlane(page_l, 0);
+  load_keys(page);
+  fetch_scales();
+  load_values(page);
+
+  // ---- the rotated queries' digits, the B operand of the int8 MFMAs
+  v4i qh[R][2], ql[R][2];
+  float row_scale[R];  // of a score, in base-2 units, before the block's
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
     float x[2][16];
-    if (ok) {
-      const uint16_t* src = a.q.p + tok * a.q.row + (hk * G + row % G) * a.q.head;
-      const int64_t at = (int64_t)clamp_pos(cb.pos[tok], cb.n_pos) * kHalf + 16 * g;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint4 u = *reinterpret_cast<const uint4*>(src + 16 * g + 8 * e);
-        const uint4 v = *reinterpret_cast<const uint4*>(src + kHalf + 16 * g + 8 * e);
-        const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, vw[4] = {v.x, v.y, v.z, v.w};
-        float cs[8], sn[8];
+    for (int e = 0; e < 4; ++e) {
+      const float cs[4] = {cs4[t][e].x, cs4[t][e].y, cs4[t][e].z, cs4[t][e].w};
+      const float sn[4] = {sn4[t][e].x, sn4[t][e].y, sn4[t][e].z, sn4[t][e].w};
+      const uint4 u = qr[t][e >> 1], v = qr[t][2 + (e >> 1)];
+      const uint32_t uw[2] = {(e & 1) ? u.z : u.x, (e & 1) ? u.w : u.y}, vw[2] = {(e & 1) ? v.z : v.x, (e & 1) ? v.w : v.y};
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          *reinterpret_cast<float4*>(cs + 4 * f) = *reinterpret_cast<const float4*>(cb.rope_cos + at + 8 * e + 4 * f);
-          *reinterpret_cast<float4*>(sn + 4 * f) = *reinterpret_cast<const float4*>(cb.rope_sin + at + 8 * e + 4 * f);
-        }
-#pragma unroll
-        for (int f = 0; f < 8; ++f) {
-          const float p = (f & 1) ? bf16_hi(uw[f / 2]) : bf16_lo(uw[f / 2]);
-          const float r = (f & 1) ? bf16_hi(vw[f / 2]) : bf16_lo(vw[f / 2]);
-          x[0][8 * e + f] = p * cs[f] - r * sn[f];
-          x[1][8 * e + f] = r * cs[f] + p * sn[f];
-        }
+      for (int f = 0; f < 4; ++f) {
+        const float p = (f & 1) ? bf16_hi(uw[f / 2]) : bf16_lo(uw[f / 2]);
+        const float r = (f & 1) ? bf16_hi(vw[f / 2]) : bf16_lo(vw[f / 2]);
+        x[0][4 * e + f] = p * cs[f] - r * sn[f];
+        x[1][4 * e + f] = r * cs[f] + p * sn[f];
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[0][e] = x[1][e] = 0.0f;
     }
     float top = 0.0f;
 #pragma unroll
@@ -396,61 +451,23 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
     for (int d = 0; d < 8; ++d) acc[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // ---- the wave's blocks p = p_first + kStep i, i < count; lane j of the
-  // registers below holds what block 64 (i / 64) + j needs
-  const int p_first = p_begin + (SHARED ? wave : 0);
-  const int count = p_end > p_first ? (p_end - p_first + kStep - 1) / kStep : 0;
-  int page_l = -1;
-  float ks_l = 0.0f, vlog_l = 0.0f, vinv_l = 0.0f;
-  auto fetch_batch = [&](int i0) {
-    const int i = i0 + lane;
-    page_l = -1;
-    ks_l = vlog_l = vinv_l = 0.0f;
-    if (i < count) {
-      page_l = cb.table[(int64_t)s.b * cb.max_blocks + p_first + kStep * i];
-      if (page_l < 0 || page_l >= cb.n_pages) page_l = -1;  // no page: tokens that no row sees
-    }
-    if (page_l >= 0) {
-      const float2 sc = *reinterpret_cast<const float2*>(cb.scales + ((int64_t)page_l * cb.Hkv + hk) * 2);
-      ks_l = sc.x;
-      vlog_l = sc.y == 0.0f ? kZeroLog2 : __log2f(sc.y);
-      vinv_l = sc.y == 0.0f ? kZeroInv : 1.0f / sc.y;
-    }
-  };
-  auto resource = [&](const int8_t* codes, int page) {  // an empty one where there is no page
-    return make_rsrc(codes + ((int64_t)max(page, 0) * cb.Hkv + hk) * kPageBytes, page < 0 ? 0u : (uint32_t)kPageBytes);
-  };
-  // K: row m of tile t is token 16 (m / 4) + 4 t + m % 4, so that lane group g
-  // gets the scores of tokens 16 g + 4 t ..; V: row d, tokens 16 g ..
-  const uint32_t k_off = (uint32_t)((16 * (l16 >> 2) + (l16 & 3)) * kD + 16 * g);
-  const uint32_t v_off = (uint32_t)(l16 * kBlock + 16 * g);
-  uint4 kr[4][2], vr[8];
-  auto load_keys = [&](int page) {
-    const __amdgpu_buffer_rsrc_t r = resource(cb.k_codes, page);
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) kr[t][h] = buf_load16(r, k_off + (uint32_t)(4 * t * kD + 64 * h));
-  };
-  auto load_values = [&](int page) {
-    const __amdgpu_buffer_rsrc_t r = resource(cb.v_codes, page);
-#pragma unroll
-    for (int d = 0; d < 8; ++d) vr[d] = buf_load16(r, v_off + (uint32_t)(16 * d * kBlock));
-  };
-
-  fetch_batch(0);
-  int page = __builtin_amdgcn_readlane(page_l, 0);
-  load_keys(page);
-  load_values(page);
+  float vlog_l = 0.0f, vinv_l = 0.0f;
   for (int i = 0; i < count; ++i) {
     const int j = i & 63;
-    const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j));
+    if (j == 0) {  // the values' scales as they go into weights and total
+      vlog_l = scales_l.y == 0.0f ? kZeroLog2 : __log2f(scales_l.y);
+      vinv_l = scales_l.y == 0.0f ? kZeroInv : 1.0f / scales_l.y;
+    }
+    const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales_l.x), j));
     const float vlog = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vlog_l), j));
     const float vinv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vinv_l), j));
     const bool held = page >= 0;
-    if (j == 63) fetch_batch(i + 1);
+    if (j == 63) {
+      fetch_pages(i + 1);
+      fetch_scales();
+    }
     const int next = i + 1 < count ? __builtin_amdgcn_readlane(page_l, (i + 1) & 63) : -1;
-    const int key0 = (p_first + kStep * i) * kBlock;
+    const int key0 = (p_first + KW * i) * kBlock;
 
     // ---- scores: the high digits' sum, times 256, plus the low digits'
     v4i sc[R][4];
@@ -547,8 +564,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
     }
   };
 
-  if constexpr (SHARED) {
-    // the four waves' partial results of the same rows meet in LDS
+  if constexpr (KW > 1) {
+    // the KW waves' partial results of the same rows meet in LDS
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       const int r = wave * kWaveRows + 16 * t + l16;
@@ -558,23 +575,24 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
       if (g == 0) l_ml[r] = make_float2(m[t], l[t]);
     }
     lds_barrier();
-    for (int i = tid; i < kWaveRows * 16; i += kAttnWaves * 64) {
-      const int r = i >> 4, d = (i & 15) * 8;
-      if (row0 + r >= n_rows) continue;
+    for (int i = tid; i < kRows * 16; i += kAttnWaves * 64) {
+      const int r = i >> 4, d = (i & 15) * 8, row = s.item * kRows + r;
+      if (row >= n_rows) continue;
+      const int first = r / kWaveRows * KW * kWaveRows + r % kWaveRows;  // the row in the first of its waves
       float mx = -INFINITY, lsum = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) mx = fmaxf(mx, l_ml[w * kWaveRows + r].x);
+      for (int w = 0; w < KW; ++w) mx = fmaxf(mx, l_ml[first + w * kWaveRows].x);
       const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) {
-        const float2 ml = l_ml[w * kWaveRows + r];
+      for (int w = 0; w < KW; ++w) {
+        const float2 ml = l_ml[first + w * kWaveRows];
         const float f = __builtin_amdgcn_exp2f(ml.x - base);
         lsum = fmaf(ml.y, f, lsum);
-        const float* p = &l_o[(w * kWaveRows + r) * kPitch + d];
+        const float* p = &l_o[(first + w * kWaveRows) * kPitch + d];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(p[e], f, o[e]);
       }
-      write8(row0 + r, d, o, mx, lsum);
+      write8(row, d, o, mx, lsum);
     }
   } else {
 #pragma unroll
@@ -597,54 +615,80 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
   }
 }
 
-// Merge of the splits' partial results: a thread for 8 d of a (token, head).
-// Tokens of no sequence are left as they are.
+// Merge of the splits' partial results, [S][T][H]: P threads for 8 d of a
+// (token, head), each folding every P-th split, their results meeting in LDS.
+// (One thread for all of 64 splits took 36 us of the 79 that one token over
+// 100000 took: its reads wait for each other.)  Tokens of no sequence are
+// left as they are.
+template <int P>
 __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs a) {
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x, row = idx / (kD / 8), rows = (int64_t)a.c.T * a.H;
-  const int d = (int)(idx % (kD / 8)) * 8;
+  constexpr int kChunks = kD / 8, kRowsHere = 256 / (kChunks * P);
+  __shared__ float l_part[P > 1 ? 256 * 11 : 1];  // a thread's maximum, total and 8 sums
+  const int tid = threadIdx.x, c = tid % kChunks, part = tid / kChunks % P;
+  const int64_t row = (int64_t)blockIdx.x * kRowsHere + tid / (kChunks * P), rows = (int64_t)a.c.T * a.H;
   const int64_t tok = row / a.H;
-  if (row >= rows || tok < a.c.starts[0] || tok >= a.c.starts[a.c.B]) return;
+  const bool ok = row < rows && tok >= a.c.starts[0] && tok < a.c.starts[a.c.B];
   float mx = -INFINITY, lsum = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.S; ++s) mx = fmaxf(mx, a.part_ml[(s * rows + row) * 2]);
-  const float base = mx == -INFINITY ? 0.0f : mx;
-  for (int s = 0; s < a.S; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (s * rows + row) * 2);
-    const float f = __builtin_amdgcn_exp2f(ml.x - base);
-    lsum = fmaf(ml.y, f, lsum);
-    const float4* p = reinterpret_cast<const float4*>(a.part_o + (s * rows + row) * kD + d);
-    const float4 u = p[0], v = p[1];
-    const float w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+  auto fold = [&](float m2, float l2, const float* w) {  // one more partial result
+    const float top = fmaxf(mx, m2), base = top == -INFINITY ? 0.0f : top;
+    const float f0 = __builtin_amdgcn_exp2f(mx - base), f1 = __builtin_amdgcn_exp2f(m2 - base);
+    lsum = lsum * f0 + l2 * f1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = fmaf(w[e], f, o[e]);
+    for (int e = 0; e < 8; ++e) o[e] = o[e] * f0 + w[e] * f1;
+    mx = top;
+  };
+  if (ok)
+    for (int s = part; s < a.S; s += P) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (s * rows + row) * 2);
+      const float4* p = reinterpret_cast<const float4*>(a.part_o + (s * rows + row) * kD + 8 * c);
+      const float4 u = p[0], v = p[1];
+      const float w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+      fold(ml.x, ml.y, w);
+    }
+  if constexpr (P > 1) {
+    float* mine = l_part + tid * 11;
+    mine[0] = mx;
+    mine[1] = lsum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mine[2 + e] = o[e];
+    lds_barrier();
+    if (part != 0) return;
+    for (int q = 1; q < P; ++q) {
+      const float* p = mine + q * kChunks * 11;
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = p[2 + e];
+      fold(p[0], p[1], w);
+    }
   }
+  if (!ok) return;
   const float inv = lsum > 0.0f ? 1.0f / lsum : lsum;
-  *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + (row % a.H) * a.o.head + d) =
+  *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + (row % a.H) * a.o.head + 8 * c) =
       make_uint4(bf16x2_bits(o[0] * inv, o[1] * inv), bf16x2_bits(o[2] * inv, o[3] * inv),
                  bf16x2_bits(o[4] * inv, o[5] * inv), bf16x2_bits(o[6] * inv, o[7] * inv));
 }
 
-// The form of a call: row tiles a wave, whether the waves share rows, the
-// workgroups' number of rows, the most row blocks that the batch can have,
-// and the splits of the blocks.
+// The form of a call: row tiles a wave, waves that share rows, the
+// workgroup's rows, the most row blocks that the batch can have, and the
+// splits of the blocks.
 struct AttnPlan {
-  int R;
-  bool shared;
-  int rows;
+  int R, KW, rows;
   int64_t tiles;
   int S;
 };
 
+constexpr int kPlanLeast = 4, kPlanWgs = 512;
 AttnPlan plan_attention(int B, int T, int H, int Hkv, int max_len) {
   AttnPlan p;
   const int64_t G = H / Hkv, all = (int64_t)T * G, mean = (all + B - 1) / B;
-  p.shared = mean <= 32;
   p.R = mean <= 16 ? 1 : 2;
-  p.rows = (p.shared ? 1 : kAttnWaves) * 16 * p.R;
+  p.KW = mean <= 32 ? 4 : mean <= 64 ? 2 : 1;
+  p.rows = kAttnWaves / p.KW * 16 * p.R;
   // every sequence's last row block may be partial, but each has a row
   p.tiles = std::min<int64_t>(all / p.rows + B, T * ((G + p.rows - 1) / p.rows));
   const int64_t blocks = (max_len + kBlock - 1) / kBlock, items = std::max<int64_t>(p.tiles * Hkv, 1);
-  const int64_t least = p.shared ? 8 : 4;  // blocks of a split
-  p.S = (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + items - 1) / items, blocks / least, 64}));
+  const int64_t least = kPlanLeast;  // blocks of a split
+  p.S = (int)std::max<int64_t>(1, std::min<int64_t>({(kPlanWgs + items - 1) / items, blocks / least, 64}));
   return p;
 }
 
@@ -676,11 +720,17 @@ hipError_t launch_cache_attention(const CacheAttnArgs& a0, hipStream_t stream) {
   const int64_t grid = p.tiles * a.c.Hkv * a.S;
   if (grid > kMaxGrid) return hipErrorInvalidValue;
   typedef void (*Fn)(const CacheAttnArgs);
-  const Fn k = p.shared ? (p.R == 1 ? (Fn)cache_attention<1, true> : (Fn)cache_attention<2, true>) : (Fn)cache_attention<2, false>;
+  const Fn k = p.R == 1 ? (Fn)cache_attention<1, 4>
+               : p.KW == 4 ? (Fn)cache_attention<2, 4>
+               : p.KW == 2 ? (Fn)cache_attention<2, 2>
+                           : (Fn)cache_attention<2, 1>;
   k<<<dim3((unsigned)grid), dim3(kAttnWaves * 64), 0, stream>>>(a);
   if (a.S > 1) {
     const int64_t threads = (int64_t)a.c.T * a.H * (kD / 8);
-    cache_attention_merge<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream>>>(a);
+    if (a.S <= 4)
+      cache_attention_merge<1><<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream>>>(a);
+    else
+      cache_attention_merge<16><<<dim3((unsigned)(threads / 16)), dim3(256), 0, stream>>>(a);
   }
   return hipGetLastError();
 }
