@@ -256,10 +256,11 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kAttnWaves = 4;
-// log2 of the factor on all weights: fp16 then holds weights down to 2^-29 of
-// the largest in full precision
-constexpr float kWeightShift = 15.0f;
+// Weights are exp2(score - offset) 2^12.  The offset follows the running maximum
+// only where that has outgrown it by more than 3, so that the sums are hardly
+// ever rescaled: weights reach 2^15 at most, and fp16 holds those down to
+// 2^-26 of the offset's in full precision.
+constexpr float kWeightShift = 12.0f, kSlack = 3.0f;
 // stand-in scale of a values' block of zeros (2^-80): its weights still count
 constexpr float kZeroLog2 = -80.0f, kZeroInv = 0x1p80f;
 
@@ -296,27 +297,43 @@ __device__ __forceinline__ float fold_groups(float x, F op) {
 
 // One workgroup per (rows of one sequence's kv head, split of its blocks).
 // A row is a (new token, query head of the kv head) pair, row i G + g; a wave
-// holds R tiles of 16 rows.  KW waves hold the same rows and take every KW-th
-// block each, meeting in LDS at the end; the 4 / KW groups of waves hold
-// different rows.
+// holds R tiles of 16 rows.  Of NW waves KW hold the same rows and take every
+// KW-th block each, meeting in LDS at the end; the NW / KW of them that go
+// through the same blocks hold different rows.
 //
-// Per block of 64 tokens, with everything in registers (the page's layout is
-// the operands'):
+// Per block of 64 tokens:
 //   - the rotated query is two int8 digits of a 16-bit number on its row's
 //     scale, so S^T = K Q^T is exact int8 MFMAs on the codes as they lie in
 //     the page;
 //   - lane group g (16 lanes) holds tokens 16 g .. 16 g + 15 of its row's
-//     scores, which is what a 16-byte load of a value row [d][token] gives it;
-//   - weights exp2(score + log2(values' scale) - running maximum) in fp16
-//     with the values' codes in fp16 (exact) for O^T += V^T P^T: the values'
-//     scale is inside the weight, and comes out of the weights' total through
-//     its reciprocal.
-template <int R, int KW>
-__global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const CacheAttnArgs a) {
-  constexpr int kWaveRows = 16 * R, kRows = kAttnWaves / KW * kWaveRows;
+//     scores, which is what 16 bytes of a value row [d][token] give it;
+//   - weights exp2(score + log2(values' scale) - offset) in fp16 with the
+//     values' codes in fp16 (exact) for O^T += V^T P^T: the values' scale is
+//     inside the weight, and comes out of the weights' total through its
+//     reciprocal;
+//   - the next block's scores are formed under this block's exponentials.
+//
+// Waves that share their blocks bring each through LDS, a block ahead of its
+// use: 64 lanes that fetch operands straight from a page touch 16 rows 64
+// bytes at a time, in the page's own order an instruction covers 1 KiB.  Each
+// loads its share, rows swizzled by the fetching lanes so that the 16 rows
+// that an operand read touches at once lie on distinct banks:
+//   keys    chunk c (16 bytes) of token j at c ^ (2 (j / 16) + j / 2 % 2)
+//   values  chunk c of row d at c ^ (d / 4 % 4)
+// Two waves convert the values as they read them; four convert a share each,
+// into LDS, a quarter of the vector instructions (at R = 2 they were a third
+// of all).  A wave that has its blocks to itself (KW = NW) reads its operands
+// from memory: no barrier, and a shorter way to the first of them.
+template <int R, int KW, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArgs a) {
+  constexpr int kWaveRows = 16 * R, kSame = NW / KW, kRows = kSame * kWaveRows;
+  constexpr bool kDirect = kSame == 1, kConvert = kSame >= 4;
   constexpr int kPitch = kD + 4;  // floats of a row in the merge
-  __shared__ __align__(16) float l_o[KW > 1 ? kAttnWaves * kWaveRows * kPitch : 4];
-  __shared__ float2 l_ml[KW > 1 ? kAttnWaves * kWaveRows : 1];
+  // LDS of the waves on one block: two stages of keys, then two of values
+  constexpr int kValues = 2 * kPageBytes, kValueStage = kConvert ? 2 * kPageBytes : kPageBytes;
+  constexpr int kGroupBytes = kDirect ? 0 : kValues + 2 * kValueStage, kMergeBytes = KW > 1 ? NW * kWaveRows * kPitch * 4 : 0;
+  __shared__ __align__(16) uint8_t lds[std::max(KW * kGroupBytes, kMergeBytes)];
+  __shared__ float2 l_ml[KW > 1 ? NW * kWaveRows : 1];
 
   const CacheBatch& cb = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -326,48 +343,34 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
   const Sequence s =
       find_sequence(cb, rest / a.S, [&](int n, int) { return (int)(((int64_t)n * G + kRows - 1) / kRows); });
   if (s.b < 0) return;
-  const int kw = wave % KW, n_rows = s.n * G, row0 = s.item * kRows + wave / KW * kWaveRows;
-  // tokens that the workgroup's (the wave's) last row sees
-  auto seen_by = [&](int row) { return s.len - s.n + min(row, n_rows - 1) / G + 1; };
-  const int blocks_wg = (max(seen_by(s.item * kRows + kRows - 1), 0) + kBlock - 1) / kBlock;
-  const int per = (blocks_wg + a.S - 1) / a.S;
-  const int seen = row0 < n_rows ? max(seen_by(row0 + kWaveRows - 1), 0) : 0;
-  const int p_begin = split * per, p_end = min(p_begin + per, (seen + kBlock - 1) / kBlock);
+  const int kw = wave / kSame, same = wave % kSame;
+  const int n_rows = s.n * G, wg_row0 = s.item * kRows, row0 = wg_row0 + same * kWaveRows;
+  // Row wg_row0 + x is token i0 + (r0 + x) / G: one division for the workgroup,
+  // and a product for the small numbers (below 2^13, where the half keeps it
+  // clear of the integers by more than its rounding).
+  const int i0 = wg_row0 / G, r0 = wg_row0 - i0 * G;
+  const float inv_g = 1.0f / (float)G;
+  auto token_of = [&](int x) { return i0 + (int)(((float)(r0 + x) + 0.5f) * inv_g); };
+  // blocks that the workgroup's last row sees, and of them this split's
+  const int seen = s.len - s.n + token_of(min(wg_row0 + kRows, n_rows) - 1 - wg_row0) + 1;
+  const int blocks = (max(seen, 0) + kBlock - 1) / kBlock, per = (blocks + a.S - 1) / a.S;
+  const int p_begin = split * per, p_end = min(p_begin + per, blocks);
 
-  // ---- the wave's blocks p = p_first + KW i, i < count; lane j of the
-  // registers below holds what block 64 (i / 64) + j needs
+  // ---- the wave's blocks p_first + KW i < p_end; all waves of a workgroup
+  // that meet at barriers make the same number of rounds.  Lane j of page_l
+  // and scales_l holds what block 64 (i / 64) + j needs.
   const int p_first = p_begin + kw;
-  const int count = p_end > p_first ? (p_end - p_first + KW - 1) / KW : 0;
+  const int rounds = max(p_end - (kDirect ? p_first : p_begin) + KW - 1, 0) / KW;
   int page_l = -1;
   float2 scales_l;
   auto fetch_pages = [&](int i0) {
-    const int i = i0 + lane;
-    page_l = i < count ? cb.table[(int64_t)s.b * cb.max_blocks + p_first + KW * i] : -1;
+    const int p = p_first + KW * (i0 + lane);
+    page_l = p < p_end ? cb.table[(int64_t)s.b * cb.max_blocks + p] : -1;
     if (page_l >= cb.n_pages) page_l = -1;  // no page (as below 0): tokens that no row sees
   };
   auto fetch_scales = [&] {
     scales_l = make_float2(0.0f, 0.0f);
     if (page_l >= 0) scales_l = *reinterpret_cast<const float2*>(cb.scales + ((int64_t)page_l * cb.Hkv + hk) * 2);
-  };
-  auto resource = [&](const int8_t* codes, int page) {  // an empty one where there is no page
-    return make_rsrc(codes + ((int64_t)max(page, 0) * cb.Hkv + hk) * kPageBytes, page < 0 ? 0u : (uint32_t)kPageBytes);
-  };
-  // K: row m of tile t is token 16 (m / 4) + 4 t + m % 4, so that lane group g
-  // gets the scores of tokens 16 g + 4 t ..; V: row d, tokens 16 g ..
-  const uint32_t k_off = (uint32_t)((16 * (l16 >> 2) + (l16 & 3)) * kD + 16 * g);
-  const uint32_t v_off = (uint32_t)(l16 * kBlock + 16 * g);
-  uint4 kr[4][2], vr[8];
-  auto load_keys = [&](int page) {
-    const __amdgpu_buffer_rsrc_t r = resource(cb.k_codes, page);
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) kr[t][h] = buf_load16(r, k_off + (uint32_t)(4 * t * kD + 64 * h));
-  };
-  auto load_values = [&](int page) {
-    const __amdgpu_buffer_rsrc_t r = resource(cb.v_codes, page);
-#pragma unroll
-    for (int d = 0; d < 8; ++d) vr[d] = buf_load16(r, v_off + (uint32_t)(16 * d * kBlock));
   };
   fetch_pages(0);
 
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
   for (int t = 0; t < R; ++t) {
     const int row = row0 + 16 * t + l16;
     const bool ok = row < n_rows;
-    const int i = ok ? row / G : 0, tok = s.row0 + i;  // a row past the end reads the sequence's first
+    const int i = ok ? token_of(row - wg_row0) : 0, tok = s.row0 + i;  // a row past the end reads the sequence's first
     last_key[t] = ok ? s.len - s.n + i : -1;
     const uint16_t* src = a.q.p + tok * a.q.row + (hk * G + (ok ? row - i * G : 0)) * a.q.head + 16 * g;
     const int64_t at = (int64_t)clamp_pos(cb.pos[tok], cb.n_pos) * kHalf + 16 * g;
@@ -391,10 +394,79 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
       sn4[t][e] = *reinterpret_cast<const float4*>(cb.rope_sin + at + 4 * e);
     }
   }
-  int page = __builtin_amdgcn_readlane(page_l, 0);
-  load_keys(page);
+
+  // ---- the blocks' codes.  Operand order: keys, row m of tile t is token
+  // 16 (m / 4) + 4 t + m % 4, so that lane group g gets the scores of tokens
+  // 16 g + 4 t ..; values, row d of a tile of 16, tokens 16 g ..
+  auto page_bytes = [&](int page) { return page < 0 ? 0u : (uint32_t)kPageBytes; };  // nothing is read where there is no page
+  auto page_base = [&](const int8_t* codes, int page) {
+    return uniform_ptr(codes + ((int64_t)max(page, 0) * cb.Hkv + hk) * kPageBytes);
+  };
+  uint8_t* l_group = lds + kw * kGroupBytes;
+  const uint32_t lds_group = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)l_group;
+  constexpr int kLoads = 8 / kSame;  // KiB of a block's keys (and values) that this wave loads
+  // direct: operands
+  const uint32_t k_own = (uint32_t)((16 * (l16 >> 2) + (l16 & 3)) * kD + 16 * g), v_own = (uint32_t)(l16 * kBlock + 16 * g);
+  v4i kr[kDirect ? 4 : 1][2];
+  // through LDS: 8 tokens' keys, or a tile of the values, an instruction
+  const uint32_t k_chunk = (uint32_t)((lane & 7) ^ ((lane >> 4) & 1)), k_row = (uint32_t)(lane >> 3) * kD;
+  const uint32_t v_row = (uint32_t)((lane >> 2) * kBlock + (((lane & 3) ^ (lane >> 4)) << 4));
+  auto load_keys = [&](int i, int page) {  // block i's, through LDS: to stage i % 2
+    if constexpr (kDirect) {
+      const __amdgpu_buffer_rsrc_t r = make_rsrc(page_base(cb.k_codes, page), page_bytes(page));
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) kr[t][h] = as_v4i(buf_load16(r, k_own + (uint32_t)(4 * t * kD + 64 * h)));
+    } else {
+      const u32x4 r = make_rsrc_words(page_base(cb.k_codes, page), page_bytes(page));
+      const uint32_t dst = lds_group + (uint32_t)((i & 1) * kPageBytes);
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) {
+        const int m = same * kLoads + n;  // tokens 8 m ..
+        lds_dma16(r, uniform_u32(dst + (uint32_t)(m * 1024)), k_row + ((k_chunk ^ (uint32_t)(2 * (m >> 1))) << 4) + (uint32_t)(m * 1024), 0);
+      }
+    }
+  };
+  // values: direct, or converted: to registers; converted ones then as fp16 to
+  // LDS, the two MFMA operands (8 tokens of a lane group each) of tile d at
+  // 2 d and 2 d + 1, lane group g's row r at 16 g + (r ^ 4 g); else as they lie
+  uint4 vr[kLoads];
+  auto load_values = [&](int i, int page) {
+    if constexpr (kDirect || kConvert) {
+      const __amdgpu_buffer_rsrc_t r = make_rsrc(page_base(cb.v_codes, page), page_bytes(page));
+#pragma unroll
+      for (int d = 0; d < kLoads; ++d)
+        vr[d] = buf_load16(r, (uint32_t)((same * kLoads + d) * 1024) + (kDirect ? v_own : (uint32_t)(lane * 16)));
+    } else {
+      const u32x4 r = make_rsrc_words(page_base(cb.v_codes, page), page_bytes(page));
+      const uint32_t dst = lds_group + (uint32_t)(kValues + (i & 1) * kValueStage);
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) {
+        const uint32_t at = (uint32_t)((same * kLoads + n) * 1024);
+        lds_dma16(r, uniform_u32(dst + at), v_row + at, 0);
+      }
+    }
+  };
+  const int v_put = (lane & 3) * 256 + (((lane >> 2) ^ (4 * (lane & 3))) << 4);
+  auto stage_values = [&](int i) {
+    uint8_t* dst = l_group + kValues + (i & 1) * kValueStage + 2 * same * kLoads * 1024 + v_put;
+#pragma unroll
+    for (int d = 0; d < kLoads; ++d) {
+      *reinterpret_cast<f16x8*>(dst + 2048 * d) = codes_to_f16x8(vr[d].x, vr[d].y);
+      *reinterpret_cast<f16x8*>(dst + 2048 * d + 1024) = codes_to_f16x8(vr[d].z, vr[d].w);
+    }
+  };
+  const int k_get = (16 * (l16 >> 2) + (l16 & 3)) * kD + ((g ^ (2 * (l16 >> 2) + ((l16 >> 1) & 1))) << 4);
+  const int v_get = kConvert ? g * 256 + ((l16 ^ (4 * g)) << 4) : l16 * kBlock + ((g ^ (l16 >> 2)) << 4);
+
+  // Pages of the block at hand and the ones after it.
+  int page0 = __builtin_amdgcn_readlane(page_l, 0), page1 = __builtin_amdgcn_readlane(page_l, 1),
+      page2 = __builtin_amdgcn_readlane(page_l, 2);
+  load_keys(0, page0);
   fetch_scales();
-  load_values(page);
+  load_values(0, page0);
+  if constexpr (!kDirect) load_keys(1, page1);
 
   // ---- the rotated queries' digits, the B operand of the int8 MFMAs
   v4i qh[R][2], ql[R][2];
@@ -420,7 +492,10 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaxf(fabsf(x[0][e]), fabsf(x[1][e])));
     top = fold_groups(top, [](float p, float r) { return fmaxf(p, r); });
-    // 16 bits: |x| / sq <= 32512 = 127 * 256, half a step is 2^-16 of the row's largest
+    // 16 bits: |x| / sq <= 32512 = 127 * 256, half a step is 2^-16 of the row's
+    // largest.  The number v is rounded by an addition that leaves v + 128 in
+    // the low 16 bits: its high byte is the high digit, its low byte the low
+    // digit + 128.
     const bool zero = top < 0x1p-100f;
     const float inv = zero ? 0.0f : 32512.0f / top * a.q_sign;
     row_scale[t] = top * (1.0f / 32512.0f) * a.scale_log2e;
@@ -428,16 +503,12 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        uint32_t hi[4], lo[4];
+        uint32_t v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int v = (int)rintf(x[h][4 * w + e] * inv);
-          const int d = (v + 128) >> 8;
-          hi[e] = (uint32_t)d;
-          lo[e] = (uint32_t)(v - 256 * d);
-        }
-        qh[t][h][w] = (int)pack4(hi[0], hi[1], hi[2], hi[3]);
-        ql[t][h][w] = (int)pack4(lo[0], lo[1], lo[2], lo[3]);
+        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(fmaf(x[h][4 * w + e], inv, 12582912.0f + 128.0f));
+        const uint32_t p01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), p23 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u);
+        ql[t][h][w] = (int)(__builtin_amdgcn_perm(p23, p01, 0x05040100u) ^ 0x80808080u);
+        qh[t][h][w] = (int)__builtin_amdgcn_perm(p23, p01, 0x07060302u);
       }
   }
 
@@ -451,8 +522,47 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
     for (int d = 0; d < 8; ++d) acc[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
+  // Scores of block i: the high digits' sum, times 256, plus the low digits',
+  // in passes over several tiles, whose products do not wait for each other.
+  v4i sc[R][4];
+  auto score = [&](int i) {
+    const uint8_t* src = l_group + (i & 1) * kPageBytes;
+    constexpr int kPass = R == 1 ? 4 : 2;  // token tiles at a time: the operands' registers
+#pragma unroll
+    for (int u0 = 0; u0 < 4; u0 += kPass) {
+      v4i kf[kPass][2];
+#pragma unroll
+      for (int u = 0; u < kPass; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)  // the second half of d is 4 chunks on
+          kf[u][h] = kDirect ? kr[kDirect ? u0 + u : 0][h] : *reinterpret_cast<const v4i*>(src + (k_get ^ (64 * h)) + 4 * (u0 + u) * kD);
+#pragma unroll
+      for (int p = 0; p < 4; ++p)  // high digits of both halves of d, then low digits
+#pragma unroll
+        for (int t = 0; t < R; ++t)
+#pragma unroll
+          for (int u = 0; u < kPass; ++u) {
+            v4i& x = sc[t][u0 + u];
+            x = mfma16(kf[u][p & 1], p < 2 ? qh[t][p & 1] : ql[t][p & 1], p == 0 ? v4i{0, 0, 0, 0} : p == 2 ? x << 8 : x);
+          }
+    }
+  };
+  // Everything that this wave has loaded into LDS is there, and what it has
+  // read from LDS has arrived; the asm keeps later accesses behind it.
+  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+
+  if constexpr (!kDirect) {
+    arrived();
+    if constexpr (kConvert) {
+      stage_values(0);
+      load_values(1, page1);
+    }
+    lds_barrier();
+  }
+  score(0);
+  if constexpr (kDirect) load_keys(1, page1);
   float vlog_l = 0.0f, vinv_l = 0.0f;
-  for (int i = 0; i < count; ++i) {
+  for (int i = 0; i < rounds; ++i) {
     const int j = i & 63;
     if (j == 0) {  // the values' scales as they go into weights and total
       vlog_l = scales_l.y == 0.0f ? kZeroLog2 : __log2f(scales_l.y);
@@ -461,95 +571,133 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
     const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales_l.x), j));
     const float vlog = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vlog_l), j));
     const float vinv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vinv_l), j));
-    const bool held = page >= 0;
-    if (j == 63) {
-      fetch_pages(i + 1);
-      fetch_scales();
-    }
-    const int next = i + 1 < count ? __builtin_amdgcn_readlane(page_l, (i + 1) & 63) : -1;
+    if (j == 61) fetch_pages(i + 3);  // the next 64; their scales once this block's have been read
+    if (j == 63) fetch_scales();
+    const int page3 = __builtin_amdgcn_readlane(page_l, (i + 3) & 63);
     const int key0 = (p_first + KW * i) * kBlock;
 
-    // ---- scores: the high digits' sum, times 256, plus the low digits'
-    v4i sc[R][4];
-#pragma unroll
-    for (int t = 0; t < R; ++t)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        v4i x = mfma16(as_v4i(kr[u][0]), qh[t][0], v4i{0, 0, 0, 0});
-        x = mfma16(as_v4i(kr[u][1]), qh[t][1], x);
-        x = x << 8;
-        x = mfma16(as_v4i(kr[u][0]), ql[t][0], x);
-        sc[t][u] = mfma16(as_v4i(kr[u][1]), ql[t][1], x);
+    // Block i's values and block i + 1's keys are in LDS, and block i's keys
+    // and block i - 1's values are no longer read, as the barrier at the end
+    // of the last round says: their places are free.
+    if constexpr (!kDirect) {
+      if constexpr (kConvert) {
+        stage_values(i + 1);
+        load_values(i + 2, page2);
+      } else {
+        load_values(i + 1, page1);
       }
-    load_keys(next);
+      load_keys(i + 2, page2);
+    }
 
-    // ---- weights
-    f16x8 pw[R][2];
+    // ---- the rows' largest scores, and what turns a score into an exponent:
+    // f is the base-2 factor, above 0 so that a masked -inf stays -inf
+    float x[R][16], f[R], vl[R], vi[R], top[R];
+    bool all = true;
 #pragma unroll
     for (int t = 0; t < R; ++t) {
-      float x[16];
+      int mx = sc[t][0][0];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int e = 1; e < 16; ++e) mx = max(mx, sc[t][e >> 2][e & 3]);
+      top[t] = (float)mx;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[4 * u + r] = (float)sc[t][u][r];
-      // base-2 factor of the scores, above 0 so that a masked -inf stays -inf
-      float f = row_scale[t] * ks, vl = vlog, vi = vinv;
-      f = f < 0x1p-126f ? 0x1p-126f : f;
-      const int lim = held ? last_key[t] - key0 - 16 * g : INT_MIN;  // tokens of this lane past it are not seen
-      if (__any(lim < 15)) {
+      for (int e = 0; e < 16; ++e) x[t][e] = (float)sc[t][e >> 2][e & 3];
+      f[t] = row_scale[t] * ks;
+      f[t] = f[t] < 0x1p-126f ? 0x1p-126f : f[t];
+      vl[t] = vlog;
+      vi[t] = vinv;
+      all = all && last_key[t] >= key0 + kBlock - 1;
+    }
+    if (!__all(all) || page0 < 0) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = e <= lim ? x[e] : -INFINITY;
-        if (lim < 0) {  // nothing of the block is seen, whatever its scales hold
-          f = 1.0f;
-          vl = vi = 0.0f;
+      for (int t = 0; t < R; ++t) {
+        const int lim = page0 >= 0 ? last_key[t] - key0 - 16 * g : INT_MIN;  // tokens of this lane past it are not seen
+        top[t] = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          x[t][e] = e <= lim ? x[t][e] : -INFINITY;
+          top[t] = fmaxf(top[t], x[t][e]);
+        }
+        if (page0 < 0 || last_key[t] < key0) {  // nothing of the block is seen, whatever its scales hold
+          f[t] = 1.0f;
+          vl[t] = vi[t] = 0.0f;
         }
       }
-      float top = x[0];
+    }
+    bool outgrown = false;
 #pragma unroll
-      for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
-      top = fold_groups(fmaf(top, f, vl), [](float p, float r) { return fmaxf(p, r); });
-      if (__any(top > m[t])) {
-        const float mn = fmaxf(m[t], top);
+    for (int t = 0; t < R; ++t) {
+      top[t] = fold_groups(fmaf(top[t], f[t], vl[t]), [](float p, float r) { return fmaxf(p, r); });
+      outgrown = outgrown || top[t] > m[t] + kSlack;
+    }
+    if (__any(outgrown)) {
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        const float mn = fmaxf(m[t], top[t]);
         const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mn);
         m[t] = mn;
         l[t] *= alpha;
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
       }
-      const float off = vl + kWeightShift - (m[t] == -INFINITY ? 0.0f : m[t]);
-      float sum = 0.0f;
+    }
+
+    // ---- weights, the next block's scores under them
+    f16x8 pw[R][2];
+    score(i + 1);
+    if constexpr (kDirect) load_keys(i + 2, page2);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], f, off));
-        sum += x[e];
-      }
-      l[t] = fmaf(sum, vi, l[t]);
+    for (int t = 0; t < R; ++t) {
+      const float off = vl[t] + kWeightShift - (m[t] == -INFINITY ? 0.0f : m[t]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[t], off));
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        pw[t][h] = __builtin_bit_cast(f16x8, make_uint4(f16x2_bits(x[8 * h], x[8 * h + 1]), f16x2_bits(x[8 * h + 2], x[8 * h + 3]),
-                                                        f16x2_bits(x[8 * h + 4], x[8 * h + 5]), f16x2_bits(x[8 * h + 6], x[8 * h + 7])));
+        pw[t][h] = __builtin_bit_cast(
+            f16x8, make_uint4(f16x2_bits(x[t][8 * h], x[t][8 * h + 1]), f16x2_bits(x[t][8 * h + 2], x[t][8 * h + 3]),
+                              f16x2_bits(x[t][8 * h + 4], x[t][8 * h + 5]), f16x2_bits(x[t][8 * h + 6], x[t][8 * h + 7])));
+      // the total takes the weights before their rounding to fp16, where those
+      // of a block with small values have vanished
+      float sum[4] = {x[t][0], x[t][1], x[t][2], x[t][3]};
+#pragma unroll
+      for (int e = 4; e < 16; ++e) sum[e & 3] += x[t][e];
+      l[t] = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), vi[t], l[t]);
     }
 
     // ---- O^T += V^T P^T
+    const uint8_t* src = l_group + kValues + (i & 1) * kValueStage + v_get;
 #pragma unroll
     for (int d = 0; d < 8; ++d) {
-      const f16x8 v0 = codes_to_f16x8(vr[d].x, vr[d].y), v1 = codes_to_f16x8(vr[d].z, vr[d].w);
-#pragma unroll
-      for (int t = 0; t < R; ++t) {
-        acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[t][0], acc[t][d], 0, 0, 0);
-        acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[t][1], acc[t][d], 0, 0, 0);
+      f16x8 v0, v1;
+      if constexpr (kConvert) {
+        v0 = *reinterpret_cast<const f16x8*>(src + 2048 * d);
+        v1 = *reinterpret_cast<const f16x8*>(src + 2048 * d + 1024);
+      } else {
+        const uint4 c = kDirect ? vr[kDirect ? d : 0] : *reinterpret_cast<const uint4*>(src + 1024 * d);
+        v0 = codes_to_f16x8(c.x, c.y);
+        v1 = codes_to_f16x8(c.z, c.w);
       }
+#pragma unroll
+      for (int t = 0; t < R; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[t][0], acc[t][d], 0, 0, 0);
+#pragma unroll
+      for (int t = 0; t < R; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[t][1], acc[t][d], 0, 0, 0);
     }
-    load_values(next);
-    page = next;
+    if constexpr (kDirect) {
+      load_values(i + 1, page1);
+    } else {
+      arrived();
+      lds_barrier();
+    }
+    page0 = page1;
+    page1 = page2;
+    page2 = page3;
   }
 #pragma unroll
   for (int t = 0; t < R; ++t) l[t] = fold_groups(l[t], [](float p, float r) { return p + r; });
 
   // Where a row's result goes: its partial sums, or the output.
   auto write8 = [&](int row, int d, const float (&o)[8], float mx, float lsum) {
-    const int64_t tok = s.row0 + row / G;
-    const int h = hk * G + row % G;
+    const int i = token_of(row - wg_row0), h = hk * G + row - i * G;
+    const int64_t tok = s.row0 + i;
     if (a.S > 1) {
       const int64_t at = ((int64_t)split * cb.T + tok) * a.H + h;
       float* po = a.part_o + at * kD + d;
@@ -565,7 +713,13 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
   };
 
   if constexpr (KW > 1) {
-    // the KW waves' partial results of the same rows meet in LDS
+    // the KW waves' partial results of the same rows meet in LDS, where the
+    // stages were
+    float* l_o = reinterpret_cast<float*>(lds);
+    if constexpr (!kDirect) {
+      arrived();
+      lds_barrier();
+    }
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       const int r = wave * kWaveRows + 16 * t + l16;
@@ -575,20 +729,19 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void cache_attention(const Cach
       if (g == 0) l_ml[r] = make_float2(m[t], l[t]);
     }
     lds_barrier();
-    for (int i = tid; i < kRows * 16; i += kAttnWaves * 64) {
-      const int r = i >> 4, d = (i & 15) * 8, row = s.item * kRows + r;
+    for (int i = tid; i < kRows * 16; i += NW * 64) {
+      const int r = i >> 4, d = (i & 15) * 8, row = wg_row0 + r;  // row r lies r + kRows w rows from the first wave's
       if (row >= n_rows) continue;
-      const int first = r / kWaveRows * KW * kWaveRows + r % kWaveRows;  // the row in the first of its waves
       float mx = -INFINITY, lsum = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < KW; ++w) mx = fmaxf(mx, l_ml[first + w * kWaveRows].x);
+      for (int w = 0; w < KW; ++w) mx = fmaxf(mx, l_ml[r + w * kRows].x);
       const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
-        const float2 ml = l_ml[first + w * kWaveRows];
+        const float2 ml = l_ml[r + w * kRows];
         const float f = __builtin_amdgcn_exp2f(ml.x - base);
         lsum = fmaf(ml.y, f, lsum);
-        const float* p = &l_o[(first + w * kWaveRows) * kPitch + d];
+        const float* p = &l_o[(r + w * kRows) * kPitch + d];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(p[e], f, o[e]);
       }
@@ -627,7 +780,7 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
   const int tid = threadIdx.x, c = tid % kChunks, part = tid / kChunks % P;
   const int64_t row = (int64_t)blockIdx.x * kRowsHere + tid / (kChunks * P), rows = (int64_t)a.c.T * a.H;
   const int64_t tok = row / a.H;
-  const bool ok = row < rows && tok >= a.c.starts[0] && tok < a.c.starts[a.c.B];
+  const int first = a.c.starts[0], end = a.c.starts[a.c.B];  // needed last: nothing waits for them
   float mx = -INFINITY, lsum = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   auto fold = [&](float m2, float l2, const float* w) {  // one more partial result
     const float top = fmaxf(mx, m2), base = top == -INFINITY ? 0.0f : top;
@@ -637,7 +790,7 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
     for (int e = 0; e < 8; ++e) o[e] = o[e] * f0 + w[e] * f1;
     mx = top;
   };
-  if (ok)
+  if (row < rows)
     for (int s = part; s < a.S; s += P) {
       const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (s * rows + row) * 2);
       const float4* p = reinterpret_cast<const float4*>(a.part_o + (s * rows + row) * kD + 8 * c);
@@ -661,34 +814,43 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
       fold(p[0], p[1], w);
     }
   }
-  if (!ok) return;
+  if (row >= rows || tok < first || tok >= end) return;
   const float inv = lsum > 0.0f ? 1.0f / lsum : lsum;
   *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + (row % a.H) * a.o.head + 8 * c) =
       make_uint4(bf16x2_bits(o[0] * inv, o[1] * inv), bf16x2_bits(o[2] * inv, o[3] * inv),
                  bf16x2_bits(o[4] * inv, o[5] * inv), bf16x2_bits(o[6] * inv, o[7] * inv));
 }
 
-// The form of a call: row tiles a wave, waves that share rows, the
-// workgroup's rows, the most row blocks that the batch can have, and the
-// splits of the blocks.
+// The form of a call, and the splits of the blocks.
+typedef void (*AttnFn)(const CacheAttnArgs);
+struct AttnForm {
+  int R, KW, NW;
+  AttnFn fn;
+  int rows() const { return NW / KW * 16 * R; }
+};
+const AttnForm kForms[] = {
+    {1, 4, 4, cache_attention<1, 4, 4>}, {1, 2, 4, cache_attention<1, 2, 4>}, {1, 1, 4, cache_attention<1, 1, 4>},
+    {1, 2, 8, cache_attention<1, 2, 8>}, {2, 1, 4, cache_attention<2, 1, 4>}, {2, 2, 8, cache_attention<2, 2, 8>},
+};
 struct AttnPlan {
-  int R, KW, rows;
-  int64_t tiles;
+  int form;
+  int64_t tiles;  // the most row blocks that the batch can have
   int S;
 };
 
-constexpr int kPlanLeast = 4, kPlanWgs = 512;
+// every sequence's last row block may be partial, but each has a row
+int64_t row_blocks(int B, int T, int G, int rows) {
+  return std::min<int64_t>((int64_t)T * G / rows + B, (int64_t)T * ((G + rows - 1) / rows));
+}
+
 AttnPlan plan_attention(int B, int T, int H, int Hkv, int max_len) {
   AttnPlan p;
-  const int64_t G = H / Hkv, all = (int64_t)T * G, mean = (all + B - 1) / B;
-  p.R = mean <= 16 ? 1 : 2;
-  p.KW = mean <= 32 ? 4 : mean <= 64 ? 2 : 1;
-  p.rows = kAttnWaves / p.KW * 16 * p.R;
-  // every sequence's last row block may be partial, but each has a row
-  p.tiles = std::min<int64_t>(all / p.rows + B, T * ((G + p.rows - 1) / p.rows));
+  const int G = H / Hkv;
+  const int64_t mean = ((int64_t)T * G + B - 1) / B;
+  p.form = mean <= 16 ? 0 : mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
+  p.tiles = row_blocks(B, T, G, kForms[p.form].rows());
   const int64_t blocks = (max_len + kBlock - 1) / kBlock, items = std::max<int64_t>(p.tiles * Hkv, 1);
-  const int64_t least = kPlanLeast;  // blocks of a split
-  p.S = (int)std::max<int64_t>(1, std::min<int64_t>({(kPlanWgs + items - 1) / items, blocks / least, 64}));
+  p.S = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + items - 1) / items, blocks / 4, 64}));
   return p;
 }
 
@@ -719,18 +881,14 @@ hipError_t launch_cache_attention(const CacheAttnArgs& a0, hipStream_t stream) {
   }
   const int64_t grid = p.tiles * a.c.Hkv * a.S;
   if (grid > kMaxGrid) return hipErrorInvalidValue;
-  typedef void (*Fn)(const CacheAttnArgs);
-  const Fn k = p.R == 1 ? (Fn)cache_attention<1, 4>
-               : p.KW == 4 ? (Fn)cache_attention<2, 4>
-               : p.KW == 2 ? (Fn)cache_attention<2, 2>
-                           : (Fn)cache_attention<2, 1>;
-  k<<<dim3((unsigned)grid), dim3(kAttnWaves * 64), 0, stream>>>(a);
+  const AttnForm& form = kForms[p.form];
+  form.fn<<<dim3((unsigned)grid), dim3(form.NW * 64), 0, stream>>>(a);
   if (a.S > 1) {
     const int64_t threads = (int64_t)a.c.T * a.H * (kD / 8);
-    if (a.S <= 4)
-      cache_attention_merge<1><<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream>>>(a);
-    else
-      cache_attention_merge<16><<<dim3((unsigned)(threads / 16)), dim3(256), 0, stream>>>(a);
+    const int P = a.S <= 4 ? 1 : a.S <= 16 ? 4 : 16;
+    const dim3 grid((unsigned)((threads * P + 255) / 256));
+    const AttnFn merge = P == 1 ? cache_attention_merge<1> : P == 4 ? cache_attention_merge<4> : cache_attention_merge<16>;
+    merge<<<grid, dim3(256), 0, stream>>>(a);
   }
   return hipGetLastError();
 }
