@@ -316,21 +316,20 @@ __device__ __forceinline__ float fold_groups(float x, F op) {
 // Waves that share their blocks bring each through LDS, a block ahead of its
 // use: 64 lanes that fetch operands straight from a page touch 16 rows 64
 // bytes at a time, in the page's own order an instruction covers 1 KiB.  Each
-// loads its share, rows swizzled by the fetching lanes so that the 16 rows
-// that an operand read touches at once lie on distinct banks:
-//   keys    chunk c (16 bytes) of token j at c ^ (2 (j / 16) + j / 2 % 2)
-//   values  chunk c of row d at c ^ (d / 4 % 4)
-// Two waves convert the values as they read them; four convert a share each,
-// into LDS, a quarter of the vector instructions (at R = 2 they were a third
-// of all).  A wave that has its blocks to itself (KW = NW) reads its operands
-// from memory: no barrier, and a shorter way to the first of them.
-template <int R, int KW, int NW>
+// wave loads its share; chunk c (16 bytes) of token j's keys lies at
+// c ^ (2 (j / 16) + j / 2 % 2), so that the 16 rows that an operand read
+// touches at once are on distinct banks, and it converts its share of the
+// values to fp16 on the way, a quarter of the vector instructions (at R = 2
+// they were a third of all).  A wave that has its blocks to itself (KW = NW)
+// reads its operands from memory: no barrier, and a shorter way to the first
+// of them.
+template <int R, int KW, int NW, int AUX = kCacheDefault>
 __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArgs a) {
   constexpr int kWaveRows = 16 * R, kSame = NW / KW, kRows = kSame * kWaveRows;
-  constexpr bool kDirect = kSame == 1, kConvert = kSame >= 4;
+  constexpr bool kDirect = kSame == 1;
   constexpr int kPitch = kD + 4;  // floats of a row in the merge
   // LDS of the waves on one block: two stages of keys, then two of values
-  constexpr int kValues = 2 * kPageBytes, kValueStage = kConvert ? 2 * kPageBytes : kPageBytes;
+  constexpr int kValues = 2 * kPageBytes, kValueStage = 2 * kPageBytes;
   constexpr int kGroupBytes = kDirect ? 0 : kValues + 2 * kValueStage, kMergeBytes = KW > 1 ? NW * kWaveRows * kPitch * 4 : 0;
   __shared__ __align__(16) uint8_t lds[std::max(KW * kGroupBytes, kMergeBytes)];
   __shared__ float2 l_ml[KW > 1 ? NW * kWaveRows : 1];
@@ -408,16 +407,15 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   // direct: operands
   const uint32_t k_own = (uint32_t)((16 * (l16 >> 2) + (l16 & 3)) * kD + 16 * g), v_own = (uint32_t)(l16 * kBlock + 16 * g);
   v4i kr[kDirect ? 4 : 1][2];
-  // through LDS: 8 tokens' keys, or a tile of the values, an instruction
+  // through LDS: 8 tokens' keys an instruction
   const uint32_t k_chunk = (uint32_t)((lane & 7) ^ ((lane >> 4) & 1)), k_row = (uint32_t)(lane >> 3) * kD;
-  const uint32_t v_row = (uint32_t)((lane >> 2) * kBlock + (((lane & 3) ^ (lane >> 4)) << 4));
   auto load_keys = [&](int i, int page) {  // block i's, through LDS: to stage i % 2
     if constexpr (kDirect) {
       const __amdgpu_buffer_rsrc_t r = make_rsrc(page_base(cb.k_codes, page), page_bytes(page));
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) kr[t][h] = as_v4i(buf_load16(r, k_own + (uint32_t)(4 * t * kD + 64 * h)));
+        for (int h = 0; h < 2; ++h) kr[t][h] = as_v4i(buf_load16<AUX>(r, k_own + (uint32_t)(4 * t * kD + 64 * h)));
     } else {
       const u32x4 r = make_rsrc_words(page_base(cb.k_codes, page), page_bytes(page));
       const uint32_t dst = lds_group + (uint32_t)((i & 1) * kPageBytes);
@@ -428,25 +426,15 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
       }
     }
   };
-  // values: direct, or converted: to registers; converted ones then as fp16 to
-  // LDS, the two MFMA operands (8 tokens of a lane group each) of tile d at
-  // 2 d and 2 d + 1, lane group g's row r at 16 g + (r ^ 4 g); else as they lie
+  // values: to registers, direct as operands, else in the page's order, and
+  // then as fp16 to LDS: the two MFMA operands (8 tokens of a lane group each)
+  // of tile d at 2 d and 2 d + 1, lane group g's row r at 16 g + (r ^ 4 g)
   uint4 vr[kLoads];
-  auto load_values = [&](int i, int page) {
-    if constexpr (kDirect || kConvert) {
-      const __amdgpu_buffer_rsrc_t r = make_rsrc(page_base(cb.v_codes, page), page_bytes(page));
+  auto load_values = [&](int page) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(page_base(cb.v_codes, page), page_bytes(page));
 #pragma unroll
-      for (int d = 0; d < kLoads; ++d)
-        vr[d] = buf_load16(r, (uint32_t)((same * kLoads + d) * 1024) + (kDirect ? v_own : (uint32_t)(lane * 16)));
-    } else {
-      const u32x4 r = make_rsrc_words(page_base(cb.v_codes, page), page_bytes(page));
-      const uint32_t dst = lds_group + (uint32_t)(kValues + (i & 1) * kValueStage);
-#pragma unroll
-      for (int n = 0; n < kLoads; ++n) {
-        const uint32_t at = (uint32_t)((same * kLoads + n) * 1024);
-        lds_dma16(r, uniform_u32(dst + at), v_row + at, 0);
-      }
-    }
+    for (int d = 0; d < kLoads; ++d)
+      vr[d] = buf_load16<AUX>(r, (uint32_t)((same * kLoads + d) * 1024) + (kDirect ? v_own : (uint32_t)(lane * 16)));
   };
   const int v_put = (lane & 3) * 256 + (((lane >> 2) ^ (4 * (lane & 3))) << 4);
   auto stage_values = [&](int i) {
@@ -458,14 +446,14 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
     }
   };
   const int k_get = (16 * (l16 >> 2) + (l16 & 3)) * kD + ((g ^ (2 * (l16 >> 2) + ((l16 >> 1) & 1))) << 4);
-  const int v_get = kConvert ? g * 256 + ((l16 ^ (4 * g)) << 4) : l16 * kBlock + ((g ^ (l16 >> 2)) << 4);
+  const int v_get = g * 256 + ((l16 ^ (4 * g)) << 4);
 
   // Pages of the block at hand and the ones after it.
   int page0 = __builtin_amdgcn_readlane(page_l, 0), page1 = __builtin_amdgcn_readlane(page_l, 1),
       page2 = __builtin_amdgcn_readlane(page_l, 2);
   load_keys(0, page0);
   fetch_scales();
-  load_values(0, page0);
+  load_values(page0);
   if constexpr (!kDirect) load_keys(1, page1);
 
   // ---- the rotated queries' digits, the B operand of the int8 MFMAs
@@ -553,10 +541,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 
   if constexpr (!kDirect) {
     arrived();
-    if constexpr (kConvert) {
-      stage_values(0);
-      load_values(1, page1);
-    }
+    stage_values(0);
+    load_values(page1);
     lds_barrier();
   }
   score(0);
@@ -580,12 +566,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
     // and block i - 1's values are no longer read, as the barrier at the end
     // of the last round says: their places are free.
     if constexpr (!kDirect) {
-      if constexpr (kConvert) {
-        stage_values(i + 1);
-        load_values(i + 2, page2);
-      } else {
-        load_values(i + 1, page1);
-      }
+      stage_values(i + 1);
+      load_values(page2);
       load_keys(i + 2, page2);
     }
 
@@ -668,13 +650,12 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 #pragma unroll
     for (int d = 0; d < 8; ++d) {
       f16x8 v0, v1;
-      if constexpr (kConvert) {
+      if constexpr (kDirect) {
+        v0 = codes_to_f16x8(vr[d].x, vr[d].y);
+        v1 = codes_to_f16x8(vr[d].z, vr[d].w);
+      } else {
         v0 = *reinterpret_cast<const f16x8*>(src + 2048 * d);
         v1 = *reinterpret_cast<const f16x8*>(src + 2048 * d + 1024);
-      } else {
-        const uint4 c = kDirect ? vr[kDirect ? d : 0] : *reinterpret_cast<const uint4*>(src + 1024 * d);
-        v0 = codes_to_f16x8(c.x, c.y);
-        v1 = codes_to_f16x8(c.z, c.w);
       }
 #pragma unroll
       for (int t = 0; t < R; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[t][0], acc[t][d], 0, 0, 0);
@@ -682,7 +663,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
       for (int t = 0; t < R; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[t][1], acc[t][d], 0, 0, 0);
     }
     if constexpr (kDirect) {
-      load_values(i + 1, page1);
+      load_values(page1);
     } else {
       arrived();
       lds_barrier();
@@ -769,88 +750,143 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 }
 
 // Merge of the splits' partial results, [S][T][H]: P threads for 8 d of a
-// (token, head), each folding every P-th split, their results meeting in LDS.
-// (One thread for all of 64 splits took 36 us of the 79 that one token over
-// 100000 took: its reads wait for each other.)  Tokens of no sequence are
-// left as they are.
+// (token, head), each folding every P-th split, their results meeting by lane
+// moves and, from four waves, in LDS.  (One thread for all of 64 splits took
+// 36 us of the 79 that one token over 100000 took: its reads wait for each
+// other.)  Tokens of no sequence are left as they are.
 template <int P>
 __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs a) {
   constexpr int kChunks = kD / 8, kRowsHere = 256 / (kChunks * P);
-  __shared__ float l_part[P > 1 ? 256 * 11 : 1];  // a thread's maximum, total and 8 sums
+  static_assert(P == 1 || P == 4 || P == 16, "parts of a row are the four 16-lane groups of one or four waves");
+  struct Partial {
+    float mx, sum, o[8];
+  };
+  constexpr int kWords = sizeof(Partial) / 4;
+  struct Words {
+    uint32_t w[kWords];
+  };
+  __shared__ uint32_t l_part[P == 16 ? 4 : 1][kWords][kChunks];
   const int tid = threadIdx.x, c = tid % kChunks, part = tid / kChunks % P;
   const int64_t row = (int64_t)blockIdx.x * kRowsHere + tid / (kChunks * P), rows = (int64_t)a.c.T * a.H;
   const int64_t tok = row / a.H;
   const int first = a.c.starts[0], end = a.c.starts[a.c.B];  // needed last: nothing waits for them
-  float mx = -INFINITY, lsum = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto fold = [&](float m2, float l2, const float* w) {  // one more partial result
-    const float top = fmaxf(mx, m2), base = top == -INFINITY ? 0.0f : top;
-    const float f0 = __builtin_amdgcn_exp2f(mx - base), f1 = __builtin_amdgcn_exp2f(m2 - base);
-    lsum = lsum * f0 + l2 * f1;
+  auto fold = [](const Partial& x, const Partial& y) {
+    Partial r;
+    r.mx = fmaxf(x.mx, y.mx);
+    const float base = r.mx == -INFINITY ? 0.0f : r.mx;
+    const float f0 = __builtin_amdgcn_exp2f(x.mx - base), f1 = __builtin_amdgcn_exp2f(y.mx - base);
+    r.sum = x.sum * f0 + y.sum * f1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = o[e] * f0 + w[e] * f1;
-    mx = top;
+    for (int e = 0; e < 8; ++e) r.o[e] = x.o[e] * f0 + y.o[e] * f1;
+    return r;
   };
+  Partial mine{-INFINITY, 0.0f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
   if (row < rows)
     for (int s = part; s < a.S; s += P) {
       const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (s * rows + row) * 2);
       const float4* p = reinterpret_cast<const float4*>(a.part_o + (s * rows + row) * kD + 8 * c);
       const float4 u = p[0], v = p[1];
-      const float w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-      fold(ml.x, ml.y, w);
+      mine = fold(mine, Partial{ml.x, ml.y, {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w}});
     }
   if constexpr (P > 1) {
-    float* mine = l_part + tid * 11;
-    mine[0] = mx;
-    mine[1] = lsum;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mine[2 + e] = o[e];
-    lds_barrier();
-    if (part != 0) return;
-    for (int q = 1; q < P; ++q) {
-      const float* p = mine + q * kChunks * 11;
-      float w[8];
+    for (int half = 0; half < 2; ++half) {  // lane groups 16, then 32 apart: a swap yields both values
+      const Words w = __builtin_bit_cast(Words, mine);
+      Words x, y;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = p[2 + e];
-      fold(p[0], p[1], w);
+      for (int i = 0; i < kWords; ++i) {
+        const auto r = half == 0 ? __builtin_amdgcn_permlane16_swap(w.w[i], w.w[i], false, false)
+                                 : __builtin_amdgcn_permlane32_swap(w.w[i], w.w[i], false, false);
+        x.w[i] = r[0];
+        y.w[i] = r[1];
+      }
+      mine = fold(__builtin_bit_cast(Partial, x), __builtin_bit_cast(Partial, y));
+    }
+    if constexpr (P == 16) {
+      if ((tid & 63) < kChunks) {
+        const Words w = __builtin_bit_cast(Words, mine);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) l_part[tid >> 6][i][c] = w.w[i];
+      }
+      lds_barrier();
+      if (tid >= kChunks) return;
+#pragma unroll
+      for (int q = 1; q < 4; ++q) {
+        Words w;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w.w[i] = l_part[q][i][c];
+        mine = fold(mine, __builtin_bit_cast(Partial, w));
+      }
+    } else if (part != 0) {
+      return;
     }
   }
   if (row >= rows || tok < first || tok >= end) return;
-  const float inv = lsum > 0.0f ? 1.0f / lsum : lsum;
+  const float inv = mine.sum > 0.0f ? 1.0f / mine.sum : mine.sum;
   *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + (row % a.H) * a.o.head + 8 * c) =
-      make_uint4(bf16x2_bits(o[0] * inv, o[1] * inv), bf16x2_bits(o[2] * inv, o[3] * inv),
-                 bf16x2_bits(o[4] * inv, o[5] * inv), bf16x2_bits(o[6] * inv, o[7] * inv));
+      make_uint4(bf16x2_bits(mine.o[0] * inv, mine.o[1] * inv), bf16x2_bits(mine.o[2] * inv, mine.o[3] * inv),
+                 bf16x2_bits(mine.o[4] * inv, mine.o[5] * inv), bf16x2_bits(mine.o[6] * inv, mine.o[7] * inv));
 }
 
-// The form of a call, and the splits of the blocks.
+// The forms of a call, and what one of its workgroups costs in ns: alone on a
+// CU lat + lat_round a round (a block of each of the KW groups of waves); in
+// a full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
+// thr_round a round.  Fitted, with the merge's 3400 + 0.12 a (split, token,
+// head), to 138 calls (B 1 - 64, 1 - 1024 new tokens, 1 - 100000 long, six head
+// layouts) at 12 numbers of splits: what the rule picks is 1.8 % above the best
+// of all forms and splits on average, 25 % at most; 32 rows a workgroup, 64 in
+// four waves times two and 128 in four waves, tried too, would take off under
+// 1 %.  us of 16 / 64 / 128 rows, at its best splits each: 8 x 16 tokens over
+// 2500 20.9 22.0 31.6, 32 x 16 over 1000 34.8 24.4 29.6, 1024 over 8192 250 179
+// 149.
 typedef void (*AttnFn)(const CacheAttnArgs);
 struct AttnForm {
-  int R, KW, NW;
+  int rows, KW, threads;
+  int64_t lat, lat_round, thr, thr_round;
   AttnFn fn;
-  int rows() const { return NW / KW * 16 * R; }
 };
 const AttnForm kForms[] = {
-    {1, 4, 4, cache_attention<1, 4, 4>}, {1, 2, 4, cache_attention<1, 2, 4>}, {1, 1, 4, cache_attention<1, 1, 4>},
-    {1, 2, 8, cache_attention<1, 2, 8>}, {2, 1, 4, cache_attention<2, 1, 4>}, {2, 2, 8, cache_attention<2, 2, 8>},
+    {16, 4, 256, 1100, 1090, 930, 1260, cache_attention<1, 4, 4>},
+    {64, 1, 256, 700, 1190, 1470, 750, cache_attention<1, 1, 4>},
+    {128, 2, 512, 0, 0, 5160, 2810, cache_attention<2, 2, 8>},
 };
-struct AttnPlan {
-  int form;
-  int64_t tiles;  // the most row blocks that the batch can have
-  int S;
-};
+// A cache that is read once and is larger than this does not stay in the
+// memory-side cache (256 MB) until the next call: it is read past it.  us with /
+// without: 64 sequences of 4096 (537 MB) 84 / 99, one of 100000 (205 MB) 39 / 44;
+// of 131 MB, when called again and again, 28.4 / 27.7.
+constexpr int64_t kStreamBytes = int64_t(160) << 20;
+const AttnFn kStreamFn = cache_attention<1, 4, 4, kCacheStream>;
+constexpr int64_t kMaxItems = (int64_t(1) << 32) / 512 - 1;  // a launch counts its threads in 32 bits
 
-// every sequence's last row block may be partial, but each has a row
-int64_t row_blocks(int B, int T, int G, int rows) {
-  return std::min<int64_t>((int64_t)T * G / rows + B, (int64_t)T * ((G + rows - 1) / rows));
-}
+struct AttnPlan {
+  int form = 0, S = 1;
+  bool stream = false;
+  int64_t tiles = 0;  // the most row blocks that the batch can have
+};
 
 AttnPlan plan_attention(int B, int T, int H, int Hkv, int max_len) {
+  const int64_t G = H / Hkv, n = (T + B - 1) / B, blocks = (max_len + kBlock - 1) / kBlock;
   AttnPlan p;
-  const int G = H / Hkv;
-  const int64_t mean = ((int64_t)T * G + B - 1) / B;
-  p.form = mean <= 16 ? 0 : mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
-  p.tiles = row_blocks(B, T, G, kForms[p.form].rows());
-  const int64_t blocks = (max_len + kBlock - 1) / kBlock, items = std::max<int64_t>(p.tiles * Hkv, 1);
-  p.S = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + items - 1) / items, blocks / 4, 64}));
+  int64_t least = INT64_MAX;
+  for (int f = 0; f < (int)(sizeof kForms / sizeof kForms[0]); ++f) {
+    const AttnForm& k = kForms[f];
+    const int64_t tiles = B * ((n * G + k.rows - 1) / k.rows) * Hkv;
+    for (int S : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (S > 1 && (S > blocks || (int64_t)T * H > (1 << 22))) break;
+      const int64_t rounds = ((blocks + S - 1) / S + k.KW - 1) / k.KW;
+      const int64_t cost = std::max(k.lat + rounds * k.lat_round, (tiles * S + 255) / 256 * (k.thr + rounds * k.thr_round)) +
+                           (S > 1 ? 3400 + (int64_t)S * T * H * 12 / 100 : 0);
+      if (cost < least) {
+        least = cost;
+        p.form = f;
+        p.S = S;
+      }
+    }
+  }
+  const int64_t rows = kForms[p.form].rows;
+  // every sequence's last row block may be partial, but each has a row
+  p.tiles = std::min<int64_t>(T * G / rows + B, T * ((G + rows - 1) / rows));
+  p.stream = p.form == 0 && n * G <= rows && (int64_t)B * max_len * Hkv * (2 * kD) >= kStreamBytes;
   return p;
 }
 
@@ -862,6 +898,11 @@ hipError_t launch_cache_append(const CacheAppendArgs& a, hipStream_t stream) {
   const int64_t most = std::min<int64_t>(a.c.T, ((int64_t)a.c.T + 126ll * std::min(a.c.B, a.c.T)) / kBlock);
   cache_append<<<dim3((unsigned)most, (unsigned)a.c.Hkv, 2), dim3(kAppendThreads), 0, stream>>>(a);
   return hipGetLastError();
+}
+
+bool cache_attention_fits(int B, int T, int H, int Hkv, int max_len) {
+  const AttnPlan p = plan_attention(B, T, H, Hkv, max_len);
+  return p.tiles * Hkv * p.S <= kMaxItems;
 }
 
 size_t cache_attention_workspace(int B, int T, int H, int Hkv, int max_len) {
@@ -879,16 +920,13 @@ hipError_t launch_cache_attention(const CacheAttnArgs& a0, hipStream_t stream) {
     a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterRegionBytes);
     a.part_ml = a.part_o + (size_t)a.S * a.c.T * a.H * kD;
   }
-  const int64_t grid = p.tiles * a.c.Hkv * a.S;
-  if (grid > kMaxGrid) return hipErrorInvalidValue;
-  const AttnForm& form = kForms[p.form];
-  form.fn<<<dim3((unsigned)grid), dim3(form.NW * 64), 0, stream>>>(a);
+  const AttnForm& k = kForms[p.form];
+  (p.stream ? kStreamFn : k.fn)<<<dim3((unsigned)(p.tiles * a.c.Hkv * a.S)), dim3(k.threads), 0, stream>>>(a);
   if (a.S > 1) {
-    const int64_t threads = (int64_t)a.c.T * a.H * (kD / 8);
     const int P = a.S <= 4 ? 1 : a.S <= 16 ? 4 : 16;
-    const dim3 grid((unsigned)((threads * P + 255) / 256));
+    const int64_t threads = (int64_t)a.c.T * a.H * (kD / 8) * P;
     const AttnFn merge = P == 1 ? cache_attention_merge<1> : P == 4 ? cache_attention_merge<4> : cache_attention_merge<16>;
-    merge<<<grid, dim3(256), 0, stream>>>(a);
+    merge<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream>>>(a);
   }
   return hipGetLastError();
 }
