@@ -321,9 +321,12 @@ template <bool ADD>
 hipError_t launch_norm(const uint16_t* x, const uint16_t* residual, const uint16_t* gamma, float eps, int M, int K,
                        uint16_t* sum, int8_t* q, float* scale, hipStream_t stream) {
   if (M == 0) return hipSuccess;
-  // the quantize launcher's shapes, one workgroup of at least 128 threads per row
+  // the quantize launcher's shapes, one workgroup of at least 128 threads per
+  // row; with the addition's third stream fewer chunks a thread (us of 4 / 2 / 1
+  // at K = 4096: M = 200 5.8 4.6 4.2, 777 9.1 8.7 8.8, 1500 12.9 11.3 11.1, 4096
+  // 22.7 20.7 21.3)
   const int nchunk = K / 8;
-  const int per = M <= 64 ? 1 : 4;
+  const int per = ADD ? (M < 2048 ? 1 : 2) : M <= 64 ? 1 : 4;
   int T = 128;
   while (T < 512 && T * per < nchunk) T *= 2;
   int C = 1;
