@@ -47,6 +47,25 @@ struct CacheAppendArgs {
 };
 hipError_t launch_cache_append(const CacheAppendArgs& a, hipStream_t stream);
 
+// Division of numbers 0 <= n < 2^31 by a fixed d >= 1 as a product: with
+// l = ceil(log2 d), m = ceil(2^(31 + l) / d) < 2^32 exceeds the quotient by less
+// than 1, so n m / 2^(31 + l) exceeds n / d by less than 2^-l <= 1 / d.
+struct Divisor {
+  uint32_t d = 1, m = 0, shift = 0;
+  Divisor() = default;
+  explicit Divisor(uint32_t by) : d(by) {
+    uint32_t l = 0;
+    while ((uint64_t(1) << l) < by) ++l;
+    if (by > 1) {
+      m = (uint32_t)(((uint64_t(1) << (31 + l)) + by - 1) / by);
+      shift = l - 1;
+    }
+  }
+  __host__ __device__ int divide(int n) const {
+    return d == 1 ? n : (int)((uint32_t)(((uint64_t)(uint32_t)n * m) >> 32) >> shift);
+  }
+};
+
 struct CacheAttnArgs {
   CacheBatch c;
   TokenRows q, o;
@@ -57,6 +76,8 @@ struct CacheAttnArgs {
   void* workspace;
   // set by the launcher
   int S;                  // splits of a sequence's blocks
+  float inv_g;            // 1 / G
+  Divisor by_g, by_s;
   float* part_o;          // [S][T][H][128] unnormalized partial sums
   float* part_ml;         // [S][T][H][2] running maximum (base 2) and weight total
 };

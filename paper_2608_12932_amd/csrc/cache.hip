@@ -333,26 +333,33 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   constexpr int kGroupBytes = kDirect ? 0 : kValues + 2 * kValueStage, kMergeBytes = KW > 1 ? NW * kWaveRows * kPitch * 4 : 0;
   __shared__ __align__(16) uint8_t lds[std::max(KW * kGroupBytes, kMergeBytes)];
   __shared__ float2 l_ml[KW > 1 ? NW * kWaveRows : 1];
+  __shared__ float l_scale[kRows];  // of a row's scores, in base-2 units, before the block's
 
   const CacheBatch& cb = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int hk = blockIdx.x % cb.Hkv, rest = blockIdx.x / cb.Hkv, split = rest % a.S;
-  const int G = a.G;
+  const int G = a.G, kw = wave / kSame, same = wave % kSame;
+  // Workgroups of neighbouring kv heads go to the XCDs in turn, so that all of
+  // a head's row blocks find its pages in one L2.
+  const int hk = blockIdx.x;
+  int split = blockIdx.y, item = blockIdx.z;
+  if ((int)gridDim.y > a.S) {  // more row blocks than one axis of a launch holds
+    item += (split / a.S) * gridDim.z;
+    split %= a.S;
+  }
+
+  // ---- the workgroup's place.  A row's number wg_row0 + x is token i0 + (r0 +
+  // x) / G: one division for the workgroup, and a product for the small numbers
+  // (below 2^13, where the half keeps it clear of the integers by more than its
+  // rounding).
   const Sequence s =
-      find_sequence(cb, rest / a.S, [&](int n, int) { return (int)(((int64_t)n * G + kRows - 1) / kRows); });
+      find_sequence(cb, item, [&](int n, int) { return (int)(((uint32_t)(n * G) + kRows - 1) / kRows); });
   if (s.b < 0) return;
-  const int kw = wave / kSame, same = wave % kSame;
-  const int n_rows = s.n * G, wg_row0 = s.item * kRows, row0 = wg_row0 + same * kWaveRows;
-  // Row wg_row0 + x is token i0 + (r0 + x) / G: one division for the workgroup,
-  // and a product for the small numbers (below 2^13, where the half keeps it
-  // clear of the integers by more than its rounding).
-  const int i0 = wg_row0 / G, r0 = wg_row0 - i0 * G;
-  const float inv_g = 1.0f / (float)G;
-  auto token_of = [&](int x) { return i0 + (int)(((float)(r0 + x) + 0.5f) * inv_g); };
-  // blocks that the workgroup's last row sees, and of them this split's
+  const int n_rows = s.n * G, wg_row0 = s.item * kRows, i0 = a.by_g.divide(wg_row0), r0 = wg_row0 - i0 * G;
+  auto token_of = [&](int x) { return i0 + (int)(((float)(r0 + x) + 0.5f) * a.inv_g); };
+  // this split's blocks of those that the workgroup's last row sees
   const int seen = s.len - s.n + token_of(min(wg_row0 + kRows, n_rows) - 1 - wg_row0) + 1;
-  const int blocks = (max(seen, 0) + kBlock - 1) / kBlock, per = (blocks + a.S - 1) / a.S;
+  const int blocks = (max(seen, 0) + kBlock - 1) / kBlock, per = a.by_s.divide(blocks + a.S - 1);
   const int p_begin = split * per, p_end = min(p_begin + per, blocks);
 
   // ---- the wave's blocks p_first + KW i < p_end; all waves of a workgroup
@@ -372,27 +379,14 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
     if (page_l >= 0) scales_l = *reinterpret_cast<const float2*>(cb.scales + ((int64_t)page_l * cb.Hkv + hk) * 2);
   };
   fetch_pages(0);
-
-  // ---- this lane's rows (row l16 of each tile): the query's d = 16 g .. and
-  // 64 + 16 g .. and the table row, requested before the first block's codes
-  uint4 qr[R][4];
-  float4 cs4[R][4], sn4[R][4];
-  int last_key[R];  // the last token that the row sees, -1 for a row past the end
+  // the positions of the rows that this wave rotates, four at a time, 16 lanes
+  // to a row (past the sequence's rows the last one again)
+  constexpr int kTurns = kRows / NW / 4;
+  int pos_l[kTurns];
+  auto turn_row = [&](int t) { return (wave * kTurns + t) * 4 + g; };
+  auto turn_token = [&](int t) { return token_of(min(turn_row(t), n_rows - 1 - wg_row0)); };
 #pragma unroll
-  for (int t = 0; t < R; ++t) {
-    const int row = row0 + 16 * t + l16;
-    const bool ok = row < n_rows;
-    const int i = ok ? token_of(row - wg_row0) : 0, tok = s.row0 + i;  // a row past the end reads the sequence's first
-    last_key[t] = ok ? s.len - s.n + i : -1;
-    const uint16_t* src = a.q.p + tok * a.q.row + (hk * G + (ok ? row - i * G : 0)) * a.q.head + 16 * g;
-    const int64_t at = (int64_t)clamp_pos(cb.pos[tok], cb.n_pos) * kHalf + 16 * g;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      qr[t][e] = *reinterpret_cast<const uint4*>(src + (e >> 1) * kHalf + (e & 1) * 8);
-      cs4[t][e] = *reinterpret_cast<const float4*>(cb.rope_cos + at + 4 * e);
-      sn4[t][e] = *reinterpret_cast<const float4*>(cb.rope_sin + at + 4 * e);
-    }
-  }
+  for (int t = 0; t < kTurns; ++t) pos_l[t] = cb.pos[s.row0 + turn_token(t)];
 
   // ---- the blocks' codes.  Operand order: keys, row m of tile t is token
   // 16 (m / 4) + 4 t + m % 4, so that lane group g gets the scores of tokens
@@ -452,52 +446,90 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   int page0 = __builtin_amdgcn_readlane(page_l, 0), page1 = __builtin_amdgcn_readlane(page_l, 1),
       page2 = __builtin_amdgcn_readlane(page_l, 2);
   load_keys(0, page0);
+
+  // ---- the queries: lane l16 has d = 4 l16 .. and 64 + 4 l16 .. of a row.
+  // The workgroup rotates each row once and hands the digits round through
+  // LDS; rotated by every wave that needs it, a row took four times the vector
+  // instructions and loads of 16 rows each.
+  uint2 q_lo[kTurns], q_hi[kTurns];
+  float4 cs4[kTurns], sn4[kTurns];
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int i = turn_token(t), row = min(turn_row(t) + wg_row0, n_rows - 1);
+    const uint16_t* src = a.q.p + (s.row0 + i) * a.q.row + (hk * G + row - i * G) * a.q.head + 4 * l16;
+    const int64_t at = (int64_t)clamp_pos(pos_l[t], cb.n_pos) * kHalf + 4 * l16;
+    q_lo[t] = *reinterpret_cast<const uint2*>(src);
+    q_hi[t] = *reinterpret_cast<const uint2*>(src + kHalf);
+    cs4[t] = *reinterpret_cast<const float4*>(cb.rope_cos + at);
+    sn4[t] = *reinterpret_cast<const float4*>(cb.rope_sin + at);
+  }
   fetch_scales();
   load_values(page0);
   if constexpr (!kDirect) load_keys(1, page1);
 
-  // ---- the rotated queries' digits, the B operand of the int8 MFMAs
-  v4i qh[R][2], ql[R][2];
-  float row_scale[R];  // of a score, in base-2 units, before the block's
+  // A row's digits in LDS: 16 chunks of 16 bytes, the high digits of d = 16 c ..
+  // in chunk c, the low ones in 8 + c, chunk c of row r at c ^ (r % 16); where
+  // the merge comes later, or the values' second stages.
+  auto digits = [&](int row) {
+    return lds + (kDirect ? row * 256 : (row >> 6) * kGroupBytes + kValues + kValueStage + (row & 63) * 256);
+  };
 #pragma unroll
-  for (int t = 0; t < R; ++t) {
-    float x[2][16];
+  for (int t = 0; t < kTurns; ++t) {
+    const uint32_t pw[2] = {q_lo[t].x, q_lo[t].y}, rw[2] = {q_hi[t].x, q_hi[t].y};
+    const float cs[4] = {cs4[t].x, cs4[t].y, cs4[t].z, cs4[t].w}, sn[4] = {sn4[t].x, sn4[t].y, sn4[t].z, sn4[t].w};
+    float x[2][4];
+    uint32_t mag = 0;  // the largest magnitude, as bits, which order like the numbers, infinity and NaN above them
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float cs[4] = {cs4[t][e].x, cs4[t][e].y, cs4[t][e].z, cs4[t][e].w};
-      const float sn[4] = {sn4[t][e].x, sn4[t][e].y, sn4[t][e].z, sn4[t][e].w};
-      const uint4 u = qr[t][e >> 1], v = qr[t][2 + (e >> 1)];
-      const uint32_t uw[2] = {(e & 1) ? u.z : u.x, (e & 1) ? u.w : u.y}, vw[2] = {(e & 1) ? v.z : v.x, (e & 1) ? v.w : v.y};
-#pragma unroll
-      for (int f = 0; f < 4; ++f) {
-        const float p = (f & 1) ? bf16_hi(uw[f / 2]) : bf16_lo(uw[f / 2]);
-        const float r = (f & 1) ? bf16_hi(vw[f / 2]) : bf16_lo(vw[f / 2]);
-        x[0][4 * e + f] = p * cs[f] - r * sn[f];
-        x[1][4 * e + f] = r * cs[f] + p * sn[f];
-      }
+      const float p = (e & 1) ? bf16_hi(pw[e / 2]) : bf16_lo(pw[e / 2]);
+      const float r = (e & 1) ? bf16_hi(rw[e / 2]) : bf16_lo(rw[e / 2]);
+      x[0][e] = p * cs[e] - r * sn[e];
+      x[1][e] = r * cs[e] + p * sn[e];
+      mag = max(mag, max(__float_as_uint(x[0][e]) & 0x7FFFFFFFu, __float_as_uint(x[1][e]) & 0x7FFFFFFFu));
     }
-    float top = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaxf(fabsf(x[0][e]), fabsf(x[1][e])));
-    top = fold_groups(top, [](float p, float r) { return fmaxf(p, r); });
+    auto fold = [&](auto ctrl) { mag = max(mag, lane_move<decltype(ctrl)::value>(mag)); };
+    fold(std::integral_constant<int, kXor1>{});  // over the row's 16 lanes
+    fold(std::integral_constant<int, kXor2>{});
+    fold(std::integral_constant<int, kMirror8>{});
+    fold(std::integral_constant<int, kMirror16>{});
+    const float top = __uint_as_float(mag);
     // 16 bits: |x| / sq <= 32512 = 127 * 256, half a step is 2^-16 of the row's
     // largest.  The number v is rounded by an addition that leaves v + 128 in
     // the low 16 bits: its high byte is the high digit, its low byte the low
     // digit + 128.
-    const bool zero = top < 0x1p-100f;
-    const float inv = zero ? 0.0f : 32512.0f / top * a.q_sign;
-    row_scale[t] = top * (1.0f / 32512.0f) * a.scale_log2e;
+    const float inv = top < 0x1p-100f ? 0.0f : 32512.0f / top * a.q_sign;
+    const int row = turn_row(t);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(digits(row)) + (l16 & 3);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      uint32_t v[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t v[4];
+      for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(fmaf(x[h][e], inv, 12582912.0f + 128.0f));
+      const uint32_t p01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), p23 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u);
+      const int c = 4 * h + (l16 >> 2);
+      dst[4 * (c ^ (row & 15))] = __builtin_amdgcn_perm(p23, p01, 0x07060302u);
+      dst[4 * ((c + 8) ^ (row & 15))] = __builtin_amdgcn_perm(p23, p01, 0x05040100u) ^ 0x80808080u;
+    }
+    if (l16 == 0) l_scale[row] = top * (1.0f / 32512.0f) * a.scale_log2e;
+  }
+  lds_barrier();
+
+  // ---- this lane's rows (row l16 of each of the wave's tiles): digits, the B
+  // operand of the int8 MFMAs, d = 16 g .. and 64 + 16 g ..
+  v4i qh[R][2], ql[R][2];
+  float row_scale[R];
+  int last_key[R];  // the last token that the row sees, -1 for a row past the end
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(fmaf(x[h][4 * w + e], inv, 12582912.0f + 128.0f));
-        const uint32_t p01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), p23 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u);
-        ql[t][h][w] = (int)(__builtin_amdgcn_perm(p23, p01, 0x05040100u) ^ 0x80808080u);
-        qh[t][h][w] = (int)__builtin_amdgcn_perm(p23, p01, 0x07060302u);
-      }
+  for (int t = 0; t < R; ++t) {
+    const int row = same * kWaveRows + 16 * t + l16;
+    const uint8_t* src = digits(row);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      qh[t][h] = *reinterpret_cast<const v4i*>(src + (((4 * h + g) ^ l16) << 4));
+      ql[t][h] = *reinterpret_cast<const v4i*>(src + (((4 * h + g + 8) ^ l16) << 4));
+    }
+    row_scale[t] = l_scale[row];
+    last_key[t] = wg_row0 + row < n_rows ? s.len - s.n + token_of(row) : -1;
   }
 
   f32x4 acc[R][8];
@@ -540,7 +572,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
 
   if constexpr (!kDirect) {
-    arrived();
+    arrived();  // (the digits, too: the values' second stages are free after the barrier)
     stage_values(0);
     load_values(page1);
     lds_barrier();
@@ -614,9 +646,11 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
     if (__any(outgrown)) {
 #pragma unroll
       for (int t = 0; t < R; ++t) {
-        const float mn = fmaxf(m[t], top[t]);
-        const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mn);
-        m[t] = mn;
+        // a row's own maximum alone moves its offset: its result does not
+        // depend on the rows that share the wave
+        const bool up = top[t] > m[t] + kSlack;
+        const float alpha = up ? __builtin_amdgcn_exp2f(m[t] - top[t]) : 1.0f;
+        m[t] = up ? top[t] : m[t];
         l[t] *= alpha;
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
@@ -697,10 +731,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
     // the KW waves' partial results of the same rows meet in LDS, where the
     // stages were
     float* l_o = reinterpret_cast<float*>(lds);
-    if constexpr (!kDirect) {
-      arrived();
-      lds_barrier();
-    }
+    arrived();
+    lds_barrier();
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       const int r = wave * kWaveRows + 16 * t + l16;
@@ -731,7 +763,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   } else {
 #pragma unroll
     for (int t = 0; t < R; ++t) {
-      const int row = row0 + 16 * t + l16;
+      const int row = wg_row0 + same * kWaveRows + 16 * t + l16;
       // lane groups g and g ^ 1 trade halves, so that a lane has 8 d in a row
 #pragma unroll
       for (int d = 0; d < 8; d += 2) {
@@ -757,7 +789,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 template <int P>
 __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs a) {
   constexpr int kChunks = kD / 8, kRowsHere = 256 / (kChunks * P);
-  static_assert(P == 1 || P == 4 || P == 16, "parts of a row are the four 16-lane groups of one or four waves");
+  static_assert(P == 4 || P == 16, "parts of a row are the four 16-lane groups of one or four waves");
   struct Partial {
     float mx, sum, o[8];
   };
@@ -788,38 +820,36 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
       const float4 u = p[0], v = p[1];
       mine = fold(mine, Partial{ml.x, ml.y, {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w}});
     }
-  if constexpr (P > 1) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {  // lane groups 16, then 32 apart: a swap yields both values
+  for (int half = 0; half < 2; ++half) {  // lane groups 16, then 32 apart: a swap yields both values
+    const Words w = __builtin_bit_cast(Words, mine);
+    Words x, y;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const auto r = half == 0 ? __builtin_amdgcn_permlane16_swap(w.w[i], w.w[i], false, false)
+                               : __builtin_amdgcn_permlane32_swap(w.w[i], w.w[i], false, false);
+      x.w[i] = r[0];
+      y.w[i] = r[1];
+    }
+    mine = fold(__builtin_bit_cast(Partial, x), __builtin_bit_cast(Partial, y));
+  }
+  if constexpr (P == 16) {
+    if ((tid & 63) < kChunks) {
       const Words w = __builtin_bit_cast(Words, mine);
-      Words x, y;
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) {
-        const auto r = half == 0 ? __builtin_amdgcn_permlane16_swap(w.w[i], w.w[i], false, false)
-                                 : __builtin_amdgcn_permlane32_swap(w.w[i], w.w[i], false, false);
-        x.w[i] = r[0];
-        y.w[i] = r[1];
-      }
-      mine = fold(__builtin_bit_cast(Partial, x), __builtin_bit_cast(Partial, y));
+      for (int i = 0; i < kWords; ++i) l_part[tid >> 6][i][c] = w.w[i];
     }
-    if constexpr (P == 16) {
-      if ((tid & 63) < kChunks) {
-        const Words w = __builtin_bit_cast(Words, mine);
+    lds_barrier();
+    if (tid >= kChunks) return;
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) l_part[tid >> 6][i][c] = w.w[i];
-      }
-      lds_barrier();
-      if (tid >= kChunks) return;
+    for (int q = 1; q < 4; ++q) {
+      Words w;
 #pragma unroll
-      for (int q = 1; q < 4; ++q) {
-        Words w;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w.w[i] = l_part[q][i][c];
-        mine = fold(mine, __builtin_bit_cast(Partial, w));
-      }
-    } else if (part != 0) {
-      return;
+      for (int i = 0; i < kWords; ++i) w.w[i] = l_part[q][i][c];
+      mine = fold(mine, __builtin_bit_cast(Partial, w));
     }
+  } else if (part != 0) {
+    return;
   }
   if (row >= rows || tok < first || tok >= end) return;
   const float inv = mine.sum > 0.0f ? 1.0f / mine.sum : mine.sum;
@@ -831,14 +861,14 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
 // The forms of a call, and what one of its workgroups costs in ns: alone on a
 // CU lat + lat_round a round (a block of each of the KW groups of waves); in
 // a full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
-// thr_round a round.  Fitted, with the merge's 3400 + 0.12 a (split, token,
+// thr_round a round.  Fitted, with the merge's 1820 + 0.21 a (split, token,
 // head), to 138 calls (B 1 - 64, 1 - 1024 new tokens, 1 - 100000 long, six head
-// layouts) at 12 numbers of splits: what the rule picks is 1.8 % above the best
-// of all forms and splits on average, 25 % at most; 32 rows a workgroup, 64 in
+// layouts) at 12 numbers of splits: what the rule picks is 0.8 % above the best
+// of all forms and splits on average, 9 % at most; 32 rows a workgroup, 64 in
 // four waves times two and 128 in four waves, tried too, would take off under
 // 1 %.  us of 16 / 64 / 128 rows, at its best splits each: 8 x 16 tokens over
-// 2500 20.9 22.0 31.6, 32 x 16 over 1000 34.8 24.4 29.6, 1024 over 8192 250 179
-// 149.
+// 2500 20.4 23.2 27.6, 23 x 27 over 478 30.5 20.8 19.1, 1024 over 8192 326 195
+// 155.
 typedef void (*AttnFn)(const CacheAttnArgs);
 struct AttnForm {
   int rows, KW, threads;
@@ -846,9 +876,9 @@ struct AttnForm {
   AttnFn fn;
 };
 const AttnForm kForms[] = {
-    {16, 4, 256, 1100, 1090, 930, 1260, cache_attention<1, 4, 4>},
-    {64, 1, 256, 700, 1190, 1470, 750, cache_attention<1, 1, 4>},
-    {128, 2, 512, 0, 0, 5160, 2810, cache_attention<2, 2, 8>},
+    {16, 4, 256, 800, 970, 860, 990, cache_attention<1, 4, 4>},
+    {64, 1, 256, 1570, 1010, 1840, 720, cache_attention<1, 1, 4>},
+    {128, 2, 512, 3010, 50, 8830, 1600, cache_attention<2, 2, 8>},
 };
 // A cache that is read once and is larger than this does not stay in the
 // memory-side cache (256 MB) until the next call: it is read past it.  us with /
@@ -856,7 +886,7 @@ const AttnForm kForms[] = {
 // of 131 MB, when called again and again, 28.4 / 27.7.
 constexpr int64_t kStreamBytes = int64_t(160) << 20;
 const AttnFn kStreamFn = cache_attention<1, 4, 4, kCacheStream>;
-constexpr int64_t kMaxItems = (int64_t(1) << 32) / 512 - 1;  // a launch counts its threads in 32 bits
+constexpr int64_t kMaxAxis = 65535;  // workgroups along the second and third axis of a launch
 
 struct AttnPlan {
   int form = 0, S = 1;
@@ -875,7 +905,7 @@ AttnPlan plan_attention(int B, int T, int H, int Hkv, int max_len) {
       if (S > 1 && (S > blocks || (int64_t)T * H > (1 << 22))) break;
       const int64_t rounds = ((blocks + S - 1) / S + k.KW - 1) / k.KW;
       const int64_t cost = std::max(k.lat + rounds * k.lat_round, (tiles * S + 255) / 256 * (k.thr + rounds * k.thr_round)) +
-                           (S > 1 ? 3400 + (int64_t)S * T * H * 12 / 100 : 0);
+                           (S > 1 ? 1820 + (int64_t)S * T * H * 21 / 100 : 0);
       if (cost < least) {
         least = cost;
         p.form = f;
@@ -902,7 +932,7 @@ hipError_t launch_cache_append(const CacheAppendArgs& a, hipStream_t stream) {
 
 bool cache_attention_fits(int B, int T, int H, int Hkv, int max_len) {
   const AttnPlan p = plan_attention(B, T, H, Hkv, max_len);
-  return p.tiles * Hkv * p.S <= kMaxItems;
+  return (int64_t)T * (H / Hkv) < INT32_MAX && p.tiles <= kMaxAxis * (kMaxAxis / p.S);
 }
 
 size_t cache_attention_workspace(int B, int T, int H, int Hkv, int max_len) {
@@ -916,16 +946,20 @@ hipError_t launch_cache_attention(const CacheAttnArgs& a0, hipStream_t stream) {
   const AttnPlan p = plan_attention(a.c.B, a.c.T, a.H, a.c.Hkv, a.max_len);
   a.G = a.H / a.c.Hkv;
   a.S = p.S;
+  a.inv_g = 1.0f / (float)a.G;
+  a.by_g = Divisor(a.G);
+  a.by_s = Divisor(a.S);
   if (a.S > 1) {
     a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterRegionBytes);
     a.part_ml = a.part_o + (size_t)a.S * a.c.T * a.H * kD;
   }
   const AttnForm& k = kForms[p.form];
-  (p.stream ? kStreamFn : k.fn)<<<dim3((unsigned)(p.tiles * a.c.Hkv * a.S)), dim3(k.threads), 0, stream>>>(a);
+  const unsigned z = (unsigned)std::min<int64_t>(p.tiles, kMaxAxis), y = (unsigned)((p.tiles + z - 1) / z) * (unsigned)a.S;
+  (p.stream ? kStreamFn : k.fn)<<<dim3((unsigned)a.c.Hkv, y, z), dim3(k.threads), 0, stream>>>(a);
   if (a.S > 1) {
-    const int P = a.S <= 4 ? 1 : a.S <= 16 ? 4 : 16;
+    const int P = a.S <= 16 ? 4 : 16;
     const int64_t threads = (int64_t)a.c.T * a.H * (kD / 8) * P;
-    const AttnFn merge = P == 1 ? cache_attention_merge<1> : P == 4 ? cache_attention_merge<4> : cache_attention_merge<16>;
+    const AttnFn merge = P == 4 ? cache_attention_merge<4> : cache_attention_merge<16>;
     merge<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream>>>(a);
   }
   return hipGetLastError();

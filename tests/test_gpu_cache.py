@@ -13,13 +13,15 @@ codes stand for, the kernel
   - rounds weights to fp16, 2^-11 of each, and forms scores and exponentials
     in fp32: exponents up to a few hundred, so within 2^-14 of each weight;
   - has fp16's smallest weights: they are scaled so that the largest of
-    P_ij s_v(j) (s_v the values' scale) is 2^15, and below 2^-14 a step of
-    fp16 is 2^-24, half a step 2^-40 of the largest; with codes up to 127
-    and N keys that is N 2^-40 max_j P_ij max |v| of j's block at most.  It
-    counts in elements d where the heavy keys' values are near 0;
+    P_ij s_v(j) (s_v the values' scale) lies in [2^12, 2^15] (it starts at
+    2^12, and only one that would pass 2^15 scales them anew), and below
+    2^-14 a step of fp16 is 2^-24, so half a step, 2^-25, is 2^-37 of the
+    largest at most; with codes up to 127 and N keys that is
+    N 2^-37 max_j P_ij max |v| of j's block at most.  It counts in elements
+    d where the heavy keys' values are near 0;
   - rounds the output to bf16, 2^-8 of it.
 With B = sum_j P_ij |v_jd| and T = N max_j P_ij max |v| of j's block:
-  |o - o64| <= 2^-8 |o64| + (1 + 2^-8) ((2^-11 + 2^-14 + 2 d (1 + 2 d)) B + 2^-40 T)."""
+  |o - o64| <= 2^-8 |o64| + (1 + 2^-8) ((2^-11 + 2^-14 + 2 d (1 + 2 d)) B + 2^-37 T)."""
 import numpy as np
 import pytest
 import torch
@@ -44,7 +46,7 @@ def tolerance(o64, bnd, top, peak, k, scale):
     H = o64.shape[1]
     l1 = np.abs(k).sum(-1).max(-1, initial=0.0)[np.arange(H) // (H // len(k))]
     d = abs(scale) * top / 65024 * l1[None]
-    return 2.0 ** -8 * np.abs(o64) + (1 + 2.0 ** -8) * ((2.0 ** -11 + 2.0 ** -14 + 2 * d * (1 + 2 * d))[..., None] * bnd + 2.0 ** -40 * peak[..., None])
+    return 2.0 ** -8 * np.abs(o64) + (1 + 2.0 ** -8) * ((2.0 ** -11 + 2.0 ** -14 + 2 * d * (1 + 2 * d))[..., None] * bnd + 2.0 ** -37 * peak[..., None])
 
 
 class Model:
@@ -396,6 +398,23 @@ def test_stale_codes_and_scales_are_not_seen():
     o = m.attend(bf16_dev(q), new)
     first = 40 + (3 * BLK - 50)  # sequence 1's new tokens begin at 50; its block 3 is seen from token 192 on
     assert torch.equal(o[:first], want[:first]) and o[first:].isnan().all()
+
+
+@pytest.mark.parametrize("n", [1, 16, 150])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_queries_that_are_no_numbers(n, what):
+    # they make their own row's output NaN and no other's
+    m = Model(2, 2, 300, seed=52)
+    m.append([300, 170])
+    q = bf16_dev(m.values(2 * n, 8))
+    want = m.attend(q, [n, n]).clone()
+    bad = q.clone()
+    bad[n - 1, 5, 77] = float(what)
+    bad[n, 0, 3] = float(what)
+    o = m.attend(bad, [n, n])
+    hit = torch.zeros(2 * n, 8, dtype=torch.bool, device=dev())
+    hit[n - 1, 5] = hit[n, 0] = True
+    assert o[hit].isnan().all() and torch.equal(o[~hit], want[~hit])
 
 
 def test_pages_out_of_range_are_not_seen():
