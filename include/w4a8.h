@@ -325,7 +325,8 @@ w4a8_status w4a8_cache_append(const w4a8_cache* cache, const w4a8_batch* batch, 
  *   rounded to bf16.
  *   q            device, bf16: token t, head h at t * q_row + h * q_head
  *                elements (as k above)
- *   H            H % Hkv == 0, H <= 4096
+ *   H            H % Hkv == 0, H <= 4096; T * H / Hkv <= 2^28 (W4A8_EUNSUPPORTED
+ *                otherwise)
  *   scale        finite, of either sign or 0
  *   max_len      an upper bound of the lengths, 1 .. 64 max_blocks: it decides
  *                how the work is split, and bounds nothing else

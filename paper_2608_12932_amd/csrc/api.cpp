@@ -451,7 +451,7 @@ w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batc
   if (!(((H == 1 || o_head >= D) && (T == 1 || o_row >= (H - 1) * o_head + D)) ||
         ((T == 1 || o_row >= D) && (H == 1 || o_head >= (T - 1) * o_row + D))))
     return W4A8_EINVAL;
-  if (!cache_attention_fits(a.c.B, a.c.T, (int)H, a.c.Hkv, (int)max_len)) return W4A8_EUNSUPPORTED;
+  if (!cache_attention_fits(a.c.T, (int)H, a.c.Hkv)) return W4A8_EUNSUPPORTED;
   const size_t need = cache_attention_workspace(a.c.B, a.c.T, (int)H, a.c.Hkv, (int)max_len);
   if (need && (workspace_bytes < need || !workspace || !aligned(workspace, 256))) return W4A8_EINVAL;
   a.q = {const_cast<uint16_t*>(q), q_row, q_head};

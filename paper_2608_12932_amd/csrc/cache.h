@@ -83,6 +83,6 @@ struct CacheAttnArgs {
 };
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream);
 size_t cache_attention_workspace(int B, int T, int H, int Hkv, int max_len);
-bool cache_attention_fits(int B, int T, int H, int Hkv, int max_len);  // one launch takes the work
+bool cache_attention_fits(int T, int H, int Hkv);  // one launch takes the work
 
 }  // namespace w4a8

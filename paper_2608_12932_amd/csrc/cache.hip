@@ -578,7 +578,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
     lds_barrier();
   }
   score(0);
-  if constexpr (kDirect) load_keys(1, page1);
+  if constexpr (kDirect)
+    load_keys(1, page1);
+  else
+    lds_barrier();  // the first round loads over block 0's keys
   float vlog_l = 0.0f, vinv_l = 0.0f;
   for (int i = 0; i < rounds; ++i) {
     const int j = i & 63;
@@ -596,7 +599,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 
     // Block i's values and block i + 1's keys are in LDS, and block i's keys
     // and block i - 1's values are no longer read, as the barrier at the end
-    // of the last round says: their places are free.
+    // of the last round (before the first round, the one behind block 0's
+    // scores) says: their places are free.
     if constexpr (!kDirect) {
       stage_values(i + 1);
       load_values(page2);
@@ -930,10 +934,10 @@ hipError_t launch_cache_append(const CacheAppendArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-bool cache_attention_fits(int B, int T, int H, int Hkv, int max_len) {
-  const AttnPlan p = plan_attention(B, T, H, Hkv, max_len);
-  return (int64_t)T * (H / Hkv) < INT32_MAX && p.tiles <= kMaxAxis * (kMaxAxis / p.S);
-}
+// 2^28 rows of a kv head: the row blocks of 64 sequences, each of which may
+// claim all rows (whatever the arrays hold), then add up within 32 bits, and
+// two axes of a launch hold the row blocks of a call.
+bool cache_attention_fits(int T, int H, int Hkv) { return (int64_t)T * (H / Hkv) <= int64_t(1) << 28; }
 
 size_t cache_attention_workspace(int B, int T, int H, int Hkv, int max_len) {
   const AttnPlan p = plan_attention(B, T, H, Hkv, max_len);

@@ -95,6 +95,9 @@ def test_attention_rejections():
     # output rows that overlap: heads on heads, tokens on tokens, tokens on heads
     for orow, oh in ((4096, 0), (0, 128), (128, 128), (4096, 120), (4088, 128), (128, 1016)):
         assert call(orow=orow, oh=oh) == EINVAL, (orow, oh)
+    # 2^28 rows of a kv head: more are refused, before any memory is touched
+    for T, H, Hkv in ((1 << 20, 4096, 1), ((1 << 20) - 1, 4096, 8), (1 << 20, 514, 2)):
+        assert call(c=cache(Hkv=Hkv), b=batch(T=T), H=H, orow=H * 128) == w.W4A8_EUNSUPPORTED, (T, H, Hkv)
     # a call that splits its sequences needs the workspace
     need = w.w4a8_cache_attention_workspace_bytes(4, 8, 32, 8, 1000)
     assert need > 64 * 1024
