@@ -34,7 +34,8 @@ def check(x, r, g, label, eps=EPS):
 # every number of threads per row and chunks per thread, rows that are read
 # again from memory (K above 32768), ragged rows
 @pytest.mark.parametrize("M,K", [(1, 128), (3, 128), (1, 4096), (16, 4096), (65, 4096), (301, 4096), (1, 12288), (70, 12288), (5, 640),
-                                 (200, 1024), (130, 2048), (100, 8192), (66, 384), (2, 32768), (2, 33024), (2, 65536), (65, 65536)])
+                                 (200, 1024), (130, 2048), (100, 8192), (66, 384), (2, 32768), (2, 33024), (2, 65536), (65, 65536),
+                                 (2047, 1024), (2048, 1024), (2049, 4096), (2500, 2560)])
 def test_bit_exact(M, K):
     check(*inputs(M, K, M + K), f"M={M} K={K}")
 

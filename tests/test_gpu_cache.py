@@ -579,6 +579,99 @@ def test_graph_of_a_step():
         assert (np.abs(out.float().cpu().numpy() - o64) <= tol).all(), rep
 
 
+def test_graphs_that_share_a_workspace():
+    # two captured calls with one workspace, replayed in turn with the linear's
+    # counters in front of their partial results
+    ms = [Model(2, 1, 3000, seed=52), Model(1, 2, 2000, seed=53)]
+    new, heads = ([2], [1, 3]), (8, 4)
+    ws = w.Workspace(dev())
+    ws.get(max(w.w4a8_cache_attention_workspace_bytes(m.B, sum(n), H, m.Hkv, m.blocks * BLK) for m, n, H in zip(ms, new, heads)))
+    calls = []
+    for m, n, H in zip(ms, new, heads):
+        m.append([m.blocks * BLK - 70] * m.B)
+        q, args = torch.empty(sum(n), H, D, dtype=torch.bfloat16, device=dev()), m.batch(n)
+        assert w.w4a8_cache_attention_workspace_bytes(m.B, sum(n), H, m.Hkv, m.blocks * BLK) > 0
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            o = w.w4a8_cache_attention(q, m.cache, *args, m.dcos, m.dsin, SCALE, workspace=ws)
+        calls.append((graph, m, n, H, q, o, args))  # the graph reads all of them
+    for rep in range(6):
+        qs = [bf16_dev(m.values(sum(n), H)) for _, m, n, H, *_ in calls]
+        for (graph, _, _, _, q, _, _), new_q in zip(calls, qs):
+            q.copy_(new_q)
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, m, n, _, _, o, _), new_q in zip(calls, qs):
+            assert torch.equal(o, m.attend(new_q, n)), rep
+    assert not ws.buf[:65536].any()
+
+
+def test_rounds_past_the_pages_held_at_a_time():
+    # a workgroup holds the pages of 64 rounds: more of them, in 128 rows ..
+    m = Model(1, 1, 9100, seed=54)
+    m.append([9050])
+    q = m.values(1600, 16)
+    assert w.w4a8_cache_attention_workspace_bytes(1, 1600, 16, 1, 9152) == 0  # not split
+    o = m.attend(bf16_dev(q), [1600])
+    torch.cuda.synchronize()
+    o64, tol = m.expect(q[-6:], [6])
+    assert (np.abs(o[-6:].float().cpu().numpy() - o64) <= tol + 1e-30).all()
+    o64, tol = m.expect(q[:6], [6], lengths=[9050 - 1600 + 6])
+    assert (np.abs(o[:6].float().cpu().numpy() - o64) <= tol + 1e-30).all()
+    # .. and in 64 rows, of sequences that share their pages (a shorter length's
+    # last page still holds the tokens after it, which no row sees)
+    B, n = 256, 4
+    for L in (9050, 4400):
+        m.cut(0, L)
+        pos, tab = i32(np.tile(np.arange(L - n, L), B)), i32(np.repeat(m.table, B, 0))
+        if L == 9050:  # two splits of 71 blocks
+            assert w.w4a8_cache_attention_workspace_bytes(B, B * n, 16, 1, L) == 65536 + 2 * B * n * 16 * (D + 2) * 4
+        q = m.values(n, 16)
+        o = w.w4a8_cache_attention(bf16_dev(np.tile(q, (B, 1, 1))), m.cache, i32(np.arange(B + 1) * n), i32([L] * B), tab, pos, m.dcos,
+                                   m.dsin, SCALE, max_len=L).view(B, n, 16, D)
+        assert torch.equal(o, o[:1].expand_as(o)), L
+        o64, tol = m.expect(q, [n])
+        assert (np.abs(o[0].float().cpu().numpy() - o64) <= tol + 1e-30).all(), L
+
+
+def test_cache_that_is_read_past_the_memory_side_cache():
+    # the upper bound of the lengths decides; the sequences are short
+    m, new, H = Model(8, 3, 700, seed=56), [1, 4, 2], 32
+    m.append([700, 64, 129])
+    q, max_len = m.values(7, H), 30000
+    starts, lengths, tab, pos = m.batch(new)
+    wide = torch.full((3, -(-max_len // BLK)), -1, dtype=torch.int32, device=dev())
+    wide[:, :m.blocks] = tab
+    o64, tol = m.expect(q, new)
+    for bound in (700, max_len):
+        o = w.w4a8_cache_attention(bf16_dev(q), m.cache, starts, lengths, wide, pos, m.dcos, m.dsin, SCALE, max_len=bound)
+        assert (np.abs(o.float().cpu().numpy() - o64) <= tol + 1e-30).all(), bound
+
+
+def test_more_row_blocks_than_an_axis_of_a_launch_holds():
+    # one key each: the output is its value, whatever the query
+    B, pages = 65536, 90
+    m = Model(1, pages, 64, seed=55)
+    m.append([1] * pages)
+    new = np.ones(B, int)
+    new[::7] = 2  # the first of two tokens sees nothing
+    starts = np.concatenate([[0], np.cumsum(new)])
+    T = int(starts[-1])
+    q = bf16_dev(np.broadcast_to(m.values(1, 1), (T, 1, D)).copy())
+    seq = np.arange(B) % pages
+    o = w.w4a8_cache_attention(q, m.cache, i32(starts), i32(np.ones(B)), i32(m.table[seq]), i32(np.zeros(T)), m.dcos, m.dsin, SCALE)
+    o = o[:, 0].double().cpu().numpy()
+    kc, vc, sc, _, _ = m.held()
+    p = m.table[seq, 0]
+    v = vc[p, 0, :, 0].astype(np.float64) * sc[p, 0, 1, None]
+    last = starts[1:] - 1
+    # the weight and the total are the same number but for the rounding to
+    # fp16 (2^-11) and fp32's products (2^-14 is far above), and one to bf16
+    assert (np.abs(o[last] - v) <= (2.0 ** -8 + (1 + 2.0 ** -8) * (2.0 ** -11 + 2.0 ** -14)) * np.abs(v)).all()
+    assert (o[starts[:-1][new == 2]] == 0).all()
+
+
 def test_refusals():
     m = Model(2, 2, 64, seed=51)
     m.append([3, 2])
