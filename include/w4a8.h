@@ -300,7 +300,7 @@ typedef struct {
  *                8 (views of a fused projection's output).  Finite: a block
  *                with another value gets unspecified codes and scales
  *   slots        device, int32 [B]: the ring of each sequence, or NULL
- *                (sequence b has ring b)
+ *                (sequence b has ring b; B <= n_slots then)
  * Every sequence of a call needs pages (of the blocks that it writes) and a
  * ring of its own.  Hkv <= 4096, n_pages and n_slots below 2^31.  Does not synchronize;
  * enqueues one kernel; deterministic.

@@ -420,6 +420,7 @@ w4a8_status w4a8_cache_append(const w4a8_cache* cache, const w4a8_batch* batch, 
   if (!cache->k_recent || !cache->v_recent || !aligned(cache->k_recent, 16) || !aligned(cache->v_recent, 16))
     return W4A8_EINVAL;
   if (!valid_rows(k, k_row, k_head) || !valid_rows(v, v_row, v_head) || !aligned(slots, 4)) return W4A8_EINVAL;
+  if (!slots && batch->B > cache->n_slots) return W4A8_EINVAL;  // sequence b has ring b
   a.k = {const_cast<uint16_t*>(k), k_row, k_head};
   a.v = {const_cast<uint16_t*>(v), v_row, v_head};
   a.k_recent = cache->k_recent;
@@ -452,8 +453,6 @@ w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batc
         ((T == 1 || o_row >= D) && (H == 1 || o_head >= (T - 1) * o_row + D))))
     return W4A8_EINVAL;
   if (!cache_attention_fits(a.c.T, (int)H, a.c.Hkv)) return W4A8_EUNSUPPORTED;
-  const size_t need = cache_attention_workspace(a.c.B, a.c.T, (int)H, a.c.Hkv, (int)max_len);
-  if (need && (workspace_bytes < need || !workspace || !aligned(workspace, 256))) return W4A8_EINVAL;
   a.q = {const_cast<uint16_t*>(q), q_row, q_head};
   a.o = {o, o_row, o_head};
   a.H = (int)H;
@@ -461,8 +460,9 @@ w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batc
   a.scale_log2e = (scale == 0.0f ? 1.0f : std::fabs(scale)) * 1.4426950408889634f;
   a.q_sign = scale == 0.0f ? 0.0f : scale < 0.0f ? -1.0f : 1.0f;
   a.max_len = (int)max_len;
-  a.workspace = workspace;
-  return launch_cache_attention(a, stream) == hipSuccess ? W4A8_OK : W4A8_EHIP;
+  hipError_t error;
+  if (!launch_cache_attention(a, workspace, workspace_bytes, stream, error)) return W4A8_EINVAL;
+  return error == hipSuccess ? W4A8_OK : W4A8_EHIP;
 }
 
 size_t w4a8_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int scale_mode, int in_kind) {

@@ -73,7 +73,6 @@ struct CacheAttnArgs {
   float scale_log2e;      // |score scale| times log2(e)
   float q_sign;           // the scale's sign, 0 for a scale of 0
   int max_len;            // the longest sequence, for the choice of splits alone
-  void* workspace;
   // set by the launcher
   int S;                  // splits of a sequence's blocks
   float inv_g;            // 1 / G
@@ -81,7 +80,8 @@ struct CacheAttnArgs {
   float* part_o;          // [S][T][H][128] unnormalized partial sums
   float* part_ml;         // [S][T][H][2] running maximum (base 2) and weight total
 };
-hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream);
+// false: the workspace is none for this call, and nothing was launched
+bool launch_cache_attention(const CacheAttnArgs& a, void* workspace, size_t bytes, hipStream_t stream, hipError_t& error);
 size_t cache_attention_workspace(int B, int T, int H, int Hkv, int max_len);
 bool cache_attention_fits(int T, int H, int Hkv);  // one launch takes the work
 

@@ -69,7 +69,7 @@ def test_append_rejections():
     for over in BAD_BATCH:
         assert call(b=batch(**over)) == EINVAL, over
     for over in (dict(k=None), dict(v=None), dict(k=P(8)), dict(kr=-8), dict(kh=4), dict(vr=100), dict(vh=-128), dict(vr=1 << 41),
-                 dict(slots=P(2))):
+                 dict(slots=P(2)), dict(c=cache(slots=3))):  # (the last: four sequences, three rings, and no slots)
         assert call(**over) == EINVAL, over
     assert f(None, batch(), K, 128, 128, V, 128, 128, None, None) == EINVAL
     assert f(cache(), None, K, 128, 128, V, 128, 128, None, None) == EINVAL
