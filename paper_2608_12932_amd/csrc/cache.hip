@@ -263,8 +263,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // ever rescaled: weights reach 2^15 at most, and fp16 holds those down to
 // 2^-26 of the offset's in full precision.
 constexpr float kWeightShift = 12.0f, kSlack = 3.0f;
-// stand-in scale of a values' block of zeros (2^-80): its weights still count
-constexpr float kZeroLog2 = -80.0f, kZeroInv = 0x1p80f;
+// A weight carries its block's scale of the values.  As long as the scales lie
+// in [kLowScale, kHighScale], a weight that vanishes in fp32 (below 2^-126)
+// counts for less than 2^-58 of the total: 2^(12 - 126) of the largest weight's
+// offset, times the 2^80 that two scales can be apart.  Past that range a block
+// whose largest weight lies more than kFar below the offset adds to the total
+// apart from its weights.
+constexpr float kLowScale = 0x1p-60f, kHighScale = 0x1p20f, kFar = 100.0f;
+// stand-in scale of a values' block of zeros: its weights still count
+constexpr float kZeroLog2 = -60.0f, kZeroInv = 0x1p60f;
 
 __device__ __forceinline__ f16x2 as_f16x2(uint32_t u) { return __builtin_bit_cast(f16x2, u); }
 
@@ -585,11 +592,13 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   else
     lds_barrier();  // the first round loads over block 0's keys
   float vlog_l = 0.0f, vinv_l = 0.0f;
+  bool careful = false;  // the wave has come to a scale of values out of the range
   for (int i = 0; i < rounds; ++i) {
     const int j = i & 63;
     if (j == 0) {  // the values' scales as they go into weights and total
       vlog_l = scales_l.y == 0.0f ? kZeroLog2 : __log2f(scales_l.y);
       vinv_l = scales_l.y == 0.0f ? kZeroInv : 1.0f / scales_l.y;
+      careful = careful || __any(scales_l.y != 0.0f && !(scales_l.y >= kLowScale && scales_l.y <= kHighScale));
     }
     const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales_l.x), j));
     const float vlog = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vlog_l), j));
@@ -649,17 +658,27 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
       top[t] = fold_groups(fmaf(top[t], f[t], vl[t]), [](float p, float r) { return fmaxf(p, r); });
       outgrown = outgrown || top[t] > m[t] + kSlack;
     }
-    if (__any(outgrown)) {
+    if (__builtin_expect(careful || __any(outgrown), 0)) {
 #pragma unroll
       for (int t = 0; t < R; ++t) {
         // a row's own maximum alone moves its offset: its result does not
         // depend on the rows that share the wave
         const bool up = top[t] > m[t] + kSlack;
-        const float alpha = up ? __builtin_amdgcn_exp2f(m[t] - top[t]) : 1.0f;
+        // in two steps: where the values' scales jump the total stays in
+        // range, and the factor would not
+        const float half = up ? __builtin_amdgcn_exp2f(0.5f * (m[t] - top[t])) : 1.0f, alpha = half * half;
         m[t] = up ? top[t] : m[t];
-        l[t] *= alpha;
+        l[t] = l[t] * half * half;
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
+        if (__builtin_expect(careful, 0)) {
+          const bool apart = top[t] < m[t] - kFar;  // (a row that has seen nothing yet is not)
+          float sum = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[t][e], f[t], kWeightShift - m[t]));
+          l[t] += apart ? sum : 0.0f;
+          vi[t] = apart ? 0.0f : vi[t];
+        }
       }
     }
 
@@ -758,8 +777,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const float2 ml = l_ml[r + w * kRows];
-        const float f = __builtin_amdgcn_exp2f(ml.x - base);
-        lsum = fmaf(ml.y, f, lsum);
+        const float half = __builtin_amdgcn_exp2f(0.5f * (ml.x - base)), f = half * half;  // as above
+        lsum = fmaf(ml.y * half, half, lsum);
         const float* p = &l_o[(r + w * kRows) * kPitch + d];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(p[e], f, o[e]);
@@ -812,8 +831,10 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
     Partial r;
     r.mx = fmaxf(x.mx, y.mx);
     const float base = r.mx == -INFINITY ? 0.0f : r.mx;
-    const float f0 = __builtin_amdgcn_exp2f(x.mx - base), f1 = __builtin_amdgcn_exp2f(y.mx - base);
-    r.sum = x.sum * f0 + y.sum * f1;
+    // in two steps, as the attention moves its offset
+    const float h0 = __builtin_amdgcn_exp2f(0.5f * (x.mx - base)), h1 = __builtin_amdgcn_exp2f(0.5f * (y.mx - base));
+    const float f0 = h0 * h0, f1 = h1 * h1;
+    r.sum = x.sum * h0 * h0 + y.sum * h1 * h1;
 #pragma unroll
     for (int e = 0; e < 8; ++e) r.o[e] = x.o[e] * f0 + y.o[e] * f1;
     return r;

@@ -359,6 +359,39 @@ def test_blocks_of_differing_size(steps):
     m.check_attention(H, [20], scale=20 * SCALE, label=steps + " peaked")
 
 
+SIZES = [(None, 57), (-90, 45), (-60, 85), (-90, 98), (None, 24), (-53, 24)]  # (the last two: as far apart as the plain way holds)
+
+
+def sized_values(m, L, pair, order, blk=BLK):
+    """bf16 values [L][1][D] whose blocks are of two sizes, 2^pair (None: zeros)."""
+    blocks = -(-L // blk)
+    which = {"low first": lambda i: i >= blocks // 2, "high first": lambda i: i < blocks // 2, "in turn": lambda i: i % 2 == 1}[order]
+    size = np.array([0.0 if pair[which(i)] is None else 2.0 ** pair[which(i)] for i in range(blocks)])
+    return I.to_bf16_bits((oracle._f32(m.values(L, 1)) * np.repeat(size, blk)[:L, None, None]).astype(np.float32))
+
+
+@pytest.mark.parametrize("order", ["low first", "high first", "in turn"])
+@pytest.mark.parametrize("pair", SIZES)
+def test_values_of_very_different_size(pair, order):
+    # blocks whose values are far smaller than others' (or zero) keep their part of the softmax's total: within a
+    # wave, between the waves of a workgroup and between splits
+    for L, H, news in ((768, 4, (1, 16)), (9000, 4, (1,))):
+        m = Model(1, 1, L, seed=57)
+        m.append([L], I.to_bf16_bits((0.3 * oracle._f32(m.values(L, 1))).astype(np.float32)), sized_values(m, L, pair, order))
+        for n in news:
+            m.check_attention(H, [n], label=f"sizes {pair} {order}")
+
+
+@pytest.mark.parametrize("pair", SIZES)
+@pytest.mark.parametrize("n,H", [(150, 32), (400, 32), (768, 32)])
+def test_values_of_very_different_size_in_many_rows(n, H, pair):
+    # the forms of more rows a workgroup
+    L = 768
+    m = Model(1, 1, L, seed=58)
+    m.append([L], I.to_bf16_bits((0.3 * oracle._f32(m.values(L, 1))).astype(np.float32)), sized_values(m, L, pair, "in turn"))
+    m.check_attention(H, [n], label=f"sizes {pair}")
+
+
 def test_a_heavy_key_with_small_values():
     # nearly all weight on keys whose values are tiny (or zero): what the others add has to keep its precision
     L = 2000
