@@ -265,13 +265,17 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr float kWeightShift = 12.0f, kSlack = 3.0f;
 // A weight carries its block's scale of the values.  As long as the scales lie
 // in [kLowScale, kHighScale], a weight that vanishes in fp32 (below 2^-126)
-// counts for less than 2^-58 of the total: 2^(12 - 126) of the largest weight's
-// offset, times the 2^80 that two scales can be apart.  Past that range a block
-// whose largest weight lies more than kFar below the offset adds to the total
-// apart from its weights.
+// counts for less than 2^-58 of the total: it lies 2^138 below a weight at the
+// offset, and two scales are 2^80 apart at most.  Past that range a block whose
+// largest weight lies more than kFar below the offset adds to the total apart
+// from its weights.
 constexpr float kLowScale = 0x1p-60f, kHighScale = 0x1p20f, kFar = 100.0f;
 // stand-in scale of a values' block of zeros: its weights still count
 constexpr float kZeroLog2 = -60.0f, kZeroInv = 0x1p60f;
+// The total is held times 2^-15: a token whose weight is at the offset then adds
+// 2^-3 / scale, up to 2^97 with the smallest scale there is and the slack, so
+// that 2^30 of them stay below 2^128, and 2^-103 with a scale of 2^100.
+constexpr float kTotalUnit = 0x1p-15f, kTotalShift = kWeightShift - 15.0f;
 
 __device__ __forceinline__ f16x2 as_f16x2(uint32_t u) { return __builtin_bit_cast(f16x2, u); }
 
@@ -293,6 +297,14 @@ __device__ __forceinline__ f16x8 codes_to_f16x8(uint32_t w0, uint32_t w1) {
 __device__ __forceinline__ uint32_t f16x2_bits(float lo, float hi) {
   const float2_t v = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+// Eight elements of a row's output from its sums and total.  A row that sees
+// nothing is 0 (0 * 0), NaN stays.
+__device__ __forceinline__ uint4 output8(const float (&o)[8], float total) {
+  const float inv = total > 0.0f ? 1.0f / total : total;
+  auto two = [&](int e) { return bf16x2_bits(o[e] * kTotalUnit * inv, o[e + 1] * kTotalUnit * inv); };
+  return make_uint4(two(0), two(2), two(4), two(6));
 }
 
 // The larger (sum) of the values of lanes l, l ^ 16, l ^ 32 and l ^ 48.
@@ -597,7 +609,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
     const int j = i & 63;
     if (j == 0) {  // the values' scales as they go into weights and total
       vlog_l = scales_l.y == 0.0f ? kZeroLog2 : __log2f(scales_l.y);
-      vinv_l = scales_l.y == 0.0f ? kZeroInv : 1.0f / scales_l.y;
+      vinv_l = scales_l.y == 0.0f ? kZeroInv * kTotalUnit : kTotalUnit / scales_l.y;
       careful = careful || __any(scales_l.y != 0.0f && !(scales_l.y >= kLowScale && scales_l.y <= kHighScale));
     }
     const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales_l.x), j));
@@ -675,7 +687,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
           const bool apart = top[t] < m[t] - kFar;  // (a row that has seen nothing yet is not)
           float sum = 0.0f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[t][e], f[t], kWeightShift - m[t]));
+          for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[t][e], f[t], kTotalShift - m[t]));
           l[t] += apart ? sum : 0.0f;
           vi[t] = apart ? 0.0f : vi[t];
         }
@@ -745,10 +757,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
       *reinterpret_cast<float4*>(po + 4) = make_float4(o[4], o[5], o[6], o[7]);
       if (d == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(mx, lsum);
     } else {
-      const float inv = lsum > 0.0f ? 1.0f / lsum : lsum;  // a row that sees nothing is 0 (0 * 0), NaN stays
-      *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + h * a.o.head + d) =
-          make_uint4(bf16x2_bits(o[0] * inv, o[1] * inv), bf16x2_bits(o[2] * inv, o[3] * inv),
-                     bf16x2_bits(o[4] * inv, o[5] * inv), bf16x2_bits(o[6] * inv, o[7] * inv));
+      *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + h * a.o.head + d) = output8(o, lsum);
     }
   };
 
@@ -879,10 +888,7 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
     return;
   }
   if (row >= rows || tok < first || tok >= end) return;
-  const float inv = mine.sum > 0.0f ? 1.0f / mine.sum : mine.sum;
-  *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + (row % a.H) * a.o.head + 8 * c) =
-      make_uint4(bf16x2_bits(mine.o[0] * inv, mine.o[1] * inv), bf16x2_bits(mine.o[2] * inv, mine.o[3] * inv),
-                 bf16x2_bits(mine.o[4] * inv, mine.o[5] * inv), bf16x2_bits(mine.o[6] * inv, mine.o[7] * inv));
+  *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + (row % a.H) * a.o.head + 8 * c) = output8(mine.o, mine.sum);
 }
 
 // The forms of a call, and what one of its workgroups costs in ns: alone on a

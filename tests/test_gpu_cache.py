@@ -392,6 +392,27 @@ def test_values_of_very_different_size_in_many_rows(n, H, pair):
     m.check_attention(H, [n], label=f"sizes {pair}")
 
 
+@pytest.mark.parametrize("blocks,B", [(1 << 14, 1), (1 << 13, 64), (1 << 13, 600)])
+def test_many_tokens_with_tiny_values(blocks, B):
+    # the total counts in units of the values' scale, here the smallest: 2^19 and more equal weights have to fit it.
+    # Every block is the same page, every score 0, so the output is the mean of the page's values
+    g = np.random.Generator(np.random.PCG64(59))
+    codes = g.integers(1, 128, (D, BLK)).astype(np.int8)
+    cache = w.KVCache.empty(1, 1, 1, device=dev())
+    cache.v_codes[0, 0] = torch.from_numpy(codes).to(dev())
+    cache.k_codes.copy_(torch.from_numpy(g.integers(-127, 128, tuple(cache.k_codes.shape)).astype(np.int8)).to(dev()))
+    cache.scales[0, 0, 0], cache.scales[0, 0, 1] = 1.0, 2.0 ** -97
+    L = blocks * BLK
+    cos, sin = torch.ones(4, D // 2, device=dev()), torch.zeros(4, D // 2, device=dev())
+    q = torch.zeros(B, 4, D, dtype=torch.bfloat16, device=dev())
+    o = w.w4a8_cache_attention(q, cache, i32(np.arange(B + 1)), i32([L] * B), i32(np.zeros((B, blocks))), i32([0] * B), cos, sin, SCALE)
+    want = codes.astype(np.float64).mean(1) * 2.0 ** -97
+    # all weights are one power of two, exact in fp16, so numerators and totals are integers times a power of two, exact in
+    # fp32 below 2^24: in every wave of a split (2^17 tokens of at most 127).  Then the merges, and the rounding to bf16
+    tol = (2.0 ** -8 + 2.0 ** -14) * want
+    assert (np.abs(o.double().cpu().numpy() - want) <= tol).all()
+
+
 def test_a_heavy_key_with_small_values():
     # nearly all weight on keys whose values are tiny (or zero): what the others add has to keep its precision
     L = 2000
