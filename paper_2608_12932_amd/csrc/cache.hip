@@ -268,10 +268,15 @@ constexpr float kWeightShift = 12.0f, kSlack = 3.0f;
 // counts for less than 2^-58 of the total: it lies 2^138 below a weight at the
 // offset, and two scales are 2^80 apart at most.  Past that range a block whose
 // largest weight lies more than kFar below the offset adds to the total apart
-// from its weights.
-constexpr float kLowScale = 0x1p-60f, kHighScale = 0x1p20f, kFar = 100.0f;
+// from its weights, in rows that have seen such a scale.
+constexpr float kLowScale = 0x1p-60f, kHighScale = 0x1p20f, kLowLog2 = -60.0f, kHighLog2 = 20.0f, kFar = 100.0f;
 // stand-in scale of a values' block of zeros: its weights still count
-constexpr float kZeroLog2 = -60.0f, kZeroInv = 0x1p60f;
+constexpr float kZeroLog2 = kLowLog2, kZeroInv = 1.0f / kLowScale;
+// Exponents are score factor + (log2 of the values' scale + 12 - offset), one
+// multiply-add a weight; with offsets from here on that sum's rounding (2^-7)
+// would show, and soon pass fp16's range: there the offset is subtracted from
+// the rounded score, which is exact where it counts.
+constexpr float kLarge = 0x1p16f;
 // The total is held times 2^-15: a token whose weight is at the offset then adds
 // 2^-3 / scale, up to 2^97 with the smallest scale there is and the slack, so
 // that 2^30 of them stay below 2^128, and 2^-103 with a scale of 2^100.
@@ -604,7 +609,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   else
     lds_barrier();  // the first round loads over block 0's keys
   float vlog_l = 0.0f, vinv_l = 0.0f;
-  bool careful = false;  // the wave has come to a scale of values out of the range
+  bool careful = false;  // the wave has come to a scale of values out of the range, or to a large offset
+  bool wild[R] = {};     // the row has seen such a scale
   for (int i = 0; i < rounds; ++i) {
     const int j = i & 63;
     if (j == 0) {  // the values' scales as they go into weights and total
@@ -668,14 +674,14 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       top[t] = fold_groups(fmaf(top[t], f[t], vl[t]), [](float p, float r) { return fmaxf(p, r); });
-      outgrown = outgrown || top[t] > m[t] + kSlack;
+      outgrown = outgrown || top[t] - m[t] > kSlack;
     }
     if (__builtin_expect(careful || __any(outgrown), 0)) {
 #pragma unroll
       for (int t = 0; t < R; ++t) {
         // a row's own maximum alone moves its offset: its result does not
         // depend on the rows that share the wave
-        const bool up = top[t] > m[t] + kSlack;
+        const bool up = top[t] - m[t] > kSlack;
         // in two steps: where the values' scales jump the total stays in
         // range, and the factor would not
         const float half = up ? __builtin_amdgcn_exp2f(0.5f * (m[t] - top[t])) : 1.0f, alpha = half * half;
@@ -683,13 +689,25 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
         l[t] = l[t] * half * half;
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
+        const bool large = fabsf(m[t]) >= kLarge && m[t] != -INFINITY;
+        careful = careful || __any(large);
         if (__builtin_expect(careful, 0)) {
-          const bool apart = top[t] < m[t] - kFar;  // (a row that has seen nothing yet is not)
+          wild[t] = wild[t] || (top[t] > -INFINITY && !(vlog >= kLowLog2 && vlog <= kHighLog2));
+          const bool apart = large || (wild[t] && top[t] < m[t] - kFar);
+          const float shift = m[t] + kWeightShift - m[t];  // what the offset below becomes: 12, and m's rounding
           float sum = 0.0f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[t][e], f[t], kTotalShift - m[t]));
-          l[t] += apart ? sum : 0.0f;
-          vi[t] = apart ? 0.0f : vi[t];
+          for (int e = 0; e < 16; ++e) {
+            const float y = fmaf(x[t][e], f[t], vl[t]) - m[t];
+            sum += __builtin_amdgcn_exp2f(y - vl[t] + kTotalShift);
+            x[t][e] = apart ? y + (kWeightShift - shift) : x[t][e];
+          }
+          if (apart) {
+            l[t] += sum;
+            f[t] = 1.0f;
+            vl[t] = m[t];
+            vi[t] = 0.0f;
+          }
         }
       }
     }

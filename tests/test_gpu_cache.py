@@ -413,6 +413,40 @@ def test_many_tokens_with_tiny_values(blocks, B):
     assert (np.abs(o.double().cpu().numpy() - want) <= tol).all()
 
 
+@pytest.mark.parametrize("size", [10, 17, 18, 20, 30, 50, 90])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_large_scores(size, sign):
+    # scores up to 2^(size + 14): integers times a unit that is far above 1, so that the heaviest keys alone count, equally.
+    # Queries and keys have one element, the tables turn nothing: the query's 16 bits are exact, and so are the products
+    L, H = 640, 4
+    m = Model(1, 1, L, seed=60)
+    m.cos, m.sin = np.ones_like(m.cos), np.zeros_like(m.sin)
+    m.dcos, m.dsin = torch.from_numpy(m.cos).to(dev()), torch.from_numpy(m.sin).to(dev())
+    k = np.zeros((L, 1, D), np.float32)
+    k[:, 0, 60] = m.rng.integers(-127, 128, L)
+    if sign < 0:
+        k[:, 0, 60] = -np.abs(k[:, 0, 60]) - (k[:, 0, 60] == 0)
+    k[::BLK, 0, 60] = -127  # every block's scale is 1
+    k[[100, 333, 600], 0, 60] = np.abs(k[:, 0, 60]).max() if sign > 0 else -1
+    v = oracle._f32(m.values(L, 1)).clip(-4, 4)
+    v[::BLK, 0, 5] = 8.0  # and every block's values have the same
+    m.append([L], I.to_bf16_bits(k), I.to_bf16_bits(v))
+    for n in (1, 20, 200):
+        q = np.zeros((n, H, D), np.float32)
+        q[:, :, 60] = 2.0 ** size * np.array([1.0, 1.5, 1.25, 64.0])
+        q = I.to_bf16_bits(q)
+        print(f"[case] large scores 2^{size} sign {sign} n={n}", flush=True)
+        o = m.attend(bf16_dev(q), [n], scale=1.0).double().cpu().numpy()
+        kc, vc, sc, _, _ = m.held()
+        pages = m.table[0]
+        kk = (kc[pages].astype(np.float64) * sc[pages, :, 0, None, None]).transpose(1, 0, 2, 3).reshape(1, -1, D)
+        vv = (vc[pages].astype(np.float64) * sc[pages, :, 1, None, None]).transpose(1, 0, 3, 2).reshape(1, -1, D)
+        o64, bnd, _, peak = oracle.cache_attention(q, np.arange(n), kk, vv, m.cos, m.sin, 1.0, L - n)
+        # the bound above without the query's rounding; other keys' weights are exp(-2^10) and less
+        tol = 2.0 ** -8 * np.abs(o64) + (1 + 2.0 ** -8) * ((2.0 ** -11 + 2.0 ** -14) * bnd + 2.0 ** -37 * peak[..., None])
+        assert (np.abs(o - o64) <= tol).all()
+
+
 def test_a_heavy_key_with_small_values():
     # nearly all weight on keys whose values are tiny (or zero): what the others add has to keep its precision
     L = 2000
