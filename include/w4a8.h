@@ -279,7 +279,9 @@ typedef struct {
  * they hold then.  Values out of range reach no memory outside the buffers:
  * starts and lengths are clamped, a block whose page is outside [0, n_pages)
  * is not written and its tokens are seen by no query, and a sequence whose
- * slot is outside [0, n_slots) has no ring.
+ * slot is outside [0, n_slots) has no ring: the append leaves a block that
+ * holds older tokens as it is (its new tokens are not held), and writes the
+ * blocks that begin with a new one.
  */
 typedef struct {
   const int32_t* starts;
@@ -319,12 +321,12 @@ w4a8_status w4a8_cache_append(const w4a8_cache* cache, const w4a8_batch* batch, 
  * nothing gets 0.  Decoding is n = 1, draft verification a few tokens, a
  * prompt's chunk any number, and a batch may mix them.
  *   The rotated query is held in 16 bits relative to its largest element
- * (half a step is 2^-16 of it) and its products with the codes are exact
- * integers; softmax and sums run in fp32, the softmax weights are rounded to
- * fp16 for the product with the values (2^-11 relative; a weight times its
- * block's scale of the values that lies below 2^-26 of the row's largest such
- * product, to 2^-37 of that); the output is rounded to bf16.  Scores have to
- * lie within fp32's range, and scales of the values below 2^100.
+ *   (half a step is 2^-16 of it) and its products with the codes are exact
+ *   integers; softmax and sums run in fp32, the softmax weights are rounded to
+ *   fp16 for the product with the values (2^-11 relative; a weight times its
+ *   block's scale of the values that lies below 2^-26 of the row's largest such
+ *   product, to 2^-37 of that); the output is rounded to bf16.  Scores have to
+ *   lie within fp32's range, and scales of the values below 2^100.
  *   q            device, bf16: token t, head h at t * q_row + h * q_head
  *                elements (as k above)
  *   H            H % Hkv == 0, H <= 4096; T * H / Hkv <= 2^28 (W4A8_EUNSUPPORTED

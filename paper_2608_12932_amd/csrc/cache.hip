@@ -213,8 +213,9 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append(const CacheAppend
   }
 
   // ---- codes and scale (magnitudes below 2^-90 count as zero, which keeps
-  // the scale and its reciprocal ordinary fp32 values)
-  if (page < 0 || page >= cb.n_pages) return;
+  // the scale and its reciprocal ordinary fp32 values).  A block whose older
+  // tokens are in no ring keeps what it has.
+  if (page < 0 || page >= cb.n_pages || (old && blk == fb && !slot_ok)) return;
   const float top = bf16_lo(__builtin_amdgcn_readfirstlane(m));
   const QScale qs = qscale_from_absmax(top < 0x1p-90f ? 0.0f : top);
   const int64_t head = (int64_t)page * cb.Hkv + hk;

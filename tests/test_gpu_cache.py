@@ -236,6 +236,36 @@ def test_append_slots_and_wrong_indices():
         assert torch.equal(x.view(torch.int8), y.view(torch.int8))
 
 
+@pytest.mark.parametrize("bad", [-1, 3, 1 << 30])
+def test_append_without_a_ring(bad):
+    # the exact values of a started block's older tokens are not known: it stays as it is; blocks without older tokens are written
+    m = Model(2, 3, 300, seed=61)
+    m.append([70, 64, 130])
+    before = [t.clone() for t in m.cache]
+    lengths = [len(k) for k in m.k]
+    print(f"[case] append, slots {bad}", flush=True)
+    m.append([5, 5, 70], slots=i32([bad] * 3))
+    kept, page = [(0, 1), (2, 2)], lambda b, blk: int(m.table[b, blk])  # noqa: E731
+    written = {(1, 1): (64, 69), (2, 3): (192, 200)}
+    touched = sorted(page(b, blk) for b, blk in written)
+    for name, x, y in zip(m.cache._fields, m.cache, before):
+        x, y = x.view(torch.int8), y.view(torch.int8)
+        if name.endswith("recent"):
+            assert torch.equal(x, y), name
+            continue
+        rest = [p for p in range(len(x)) if p not in touched]
+        assert torch.equal(x[rest], y[rest]), (name, [p in [page(*i) for i in kept] for p in rest if not torch.equal(x[p], y[p])])
+    assert lengths == [70, 64, 130]
+    kc, vc, sc, _, _ = m.held()
+    for (b, blk), (lo, hi) in written.items():
+        for h in range(2):
+            for codes, x, s in ((kc[page(b, blk), h], m.k[b], sc[page(b, blk), h, 0]), (vc[page(b, blk), h].T, m.v[b], sc[page(b, blk), h, 1])):
+                want, ws = oracle.cache_block(x[lo:hi, h])
+                assert np.float32(s).view(np.uint32) == np.float32(ws).view(np.uint32)
+                np.testing.assert_array_equal(codes[:hi - lo], want)
+                assert not codes[hi - lo:].any()
+
+
 def test_append_zero_and_tiny_blocks():
     m = Model(2, 1, 130, seed=26)
     k, v = m.values(130, 2), m.values(130, 2)
