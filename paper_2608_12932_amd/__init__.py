@@ -371,6 +371,20 @@ def _workspace_ptr(workspace, need: int, device, stream):
     return _dev(buf, "workspace", torch.uint8), buf.numel()
 
 
+@contextlib.contextmanager
+def _unless_refused(workspace):
+    """A Workspace that grows inside is as it was again where the call is
+    refused: its size is asked for before the library looks at the pointers,
+    strides and scalars."""
+    state = (workspace.buf, workspace._home) if isinstance(workspace, Workspace) else None
+    try:
+        yield
+    except Exception:
+        if state is not None:
+            workspace.buf, workspace._home = state
+        raise
+
+
 def _workspace_of(workspace):
     """(buffer, the stream that its memory is ordered on, whether it is a
     Workspace's) for the native path."""
@@ -389,8 +403,9 @@ def _linear_fast(swiglu: int, x, w_packed, w_scale, N, x_scale, scale_mode, out_
     r = fast.linear(swiglu, x, w_packed, w_scale, N, x_scale, scale_mode, out_kind, out, buf, home, own)
     if type(r) is int:
         if r < 0:  # the bytes that the Workspace, on this stream or still empty, lacks
-            workspace.get(-r)
-            return _linear_fast(swiglu, x, w_packed, w_scale, N, x_scale, scale_mode, out_kind, out, workspace)
+            with _unless_refused(workspace):
+                workspace.get(-r)
+                return _linear_fast(swiglu, x, w_packed, w_scale, N, x_scale, scale_mode, out_kind, out, workspace)
         _check(r, "w4a8_linear_swiglu" if swiglu else "w4a8_linear")
     return r
 
@@ -421,10 +436,11 @@ def _linear_call(entry: str, x, w_packed, w_scale, N, out_cols, x_scale, scale_m
         raise ValueError(f"out must be [{M}][{out_cols}]")
     y_ptr = _dev(out, "out", _OUT_DTYPE[out_kind])
     need = int(getattr(lib(), entry + "_workspace_bytes")(M, N, K, scale_mode, in_kind))
-    wk_ptr, wk_bytes = _workspace_ptr(workspace, need, x.device, stream)
-    rc = getattr(lib(), entry)(x_ptr, in_kind, xs_ptr, M, K, wp_ptr, ws_ptr, scale_mode, N, y_ptr,
-                               out_kind, wk_ptr, wk_bytes, _stream(stream))
-    _check(rc, entry)
+    with _unless_refused(workspace):
+        wk_ptr, wk_bytes = _workspace_ptr(workspace, need, x.device, stream)
+        rc = getattr(lib(), entry)(x_ptr, in_kind, xs_ptr, M, K, wp_ptr, ws_ptr, scale_mode, N, y_ptr,
+                                   out_kind, wk_ptr, wk_bytes, _stream(stream))
+        _check(rc, entry)
     return out
 
 
@@ -522,13 +538,14 @@ def w4a8_stream_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos
     elif tuple(out.shape) != (H, Nq, D):
         raise ValueError(f"out must be [{H}][{Nq}][{D}]")
     need = int(lib().w4a8_stream_attention_workspace_bytes(H, Nq, Nk)) if Nq else 0
-    wk_ptr, wk_bytes = _workspace_ptr(workspace, need, q.device, stream)
-    rc = lib().w4a8_stream_attention(_dev(q, "q", torch.bfloat16), _dev(k, "k", torch.bfloat16),
-                                     _dev(v, "v", torch.bfloat16), _dev(pos_q, "pos_q", torch.int32),
-                                     _dev(pos_k, "pos_k", torch.int32), _dev(rope_cos, "rope_cos", torch.float32),
-                                     _dev(rope_sin, "rope_sin", torch.float32), rope_cos.shape[0], H, Hkv, Nq, Nk, D,
-                                     float(scale), _dev(out, "out", torch.bfloat16), wk_ptr, wk_bytes, _stream(stream))
-    _check(rc, "w4a8_stream_attention")
+    with _unless_refused(workspace):
+        wk_ptr, wk_bytes = _workspace_ptr(workspace, need, q.device, stream)
+        rc = lib().w4a8_stream_attention(_dev(q, "q", torch.bfloat16), _dev(k, "k", torch.bfloat16),
+                                         _dev(v, "v", torch.bfloat16), _dev(pos_q, "pos_q", torch.int32),
+                                         _dev(pos_k, "pos_k", torch.int32), _dev(rope_cos, "rope_cos", torch.float32),
+                                         _dev(rope_sin, "rope_sin", torch.float32), rope_cos.shape[0], H, Hkv, Nq, Nk, D,
+                                         float(scale), _dev(out, "out", torch.bfloat16), wk_ptr, wk_bytes, _stream(stream))
+        _check(rc, "w4a8_stream_attention")
     return out
 
 
@@ -663,8 +680,9 @@ def w4a8_cache_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, 
         r = (_fast or _load_fast()).cache_attention(q, cache, starts, lengths, table, pos, rope_cos, rope_sin, scale, max_len, out, buf,
                                                     home, own)
         if type(r) is int and r < 0:  # the bytes that the Workspace, on this stream or still empty, lacks
-            workspace.get(-r)
-            return w4a8_cache_attention(q, cache, starts, lengths, table, pos, rope_cos, rope_sin, scale, max_len, out, workspace)
+            with _unless_refused(workspace):
+                workspace.get(-r)
+                return w4a8_cache_attention(q, cache, starts, lengths, table, pos, rope_cos, rope_sin, scale, max_len, out, workspace)
         if r is not None:
             return r if type(r) is not int else _check(r, "w4a8_cache_attention")
     T, H = q.shape[0], q.shape[1]
@@ -675,13 +693,13 @@ def w4a8_cache_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, 
         max_len = b.max_blocks * CACHE_BLOCK
     if out is not None and out.shape != q.shape:
         raise ValueError(f"out must be [{T}][{H}][{HEAD_DIM}]")
-    with _call_on(stream, q, k_codes=cache.k_codes, v_codes=cache.v_codes, scales=cache.scales, starts=starts, lengths=lengths,
-                  table=table, pos=pos, rope_cos=rope_cos, rope_sin=rope_sin, out=out) as s:
+    with _unless_refused(workspace), _call_on(stream, q, k_codes=cache.k_codes, v_codes=cache.v_codes, scales=cache.scales, starts=starts,
+                                              lengths=lengths, table=table, pos=pos, rope_cos=rope_cos, rope_sin=rope_sin, out=out) as s:
         if out is None:
             out = torch.empty((T, H, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
         need = w4a8_cache_attention_workspace_bytes(b.B, T, H, Hkv, max_len)
         wk_ptr, wk_bytes = _workspace_ptr(workspace, need, q.device, s)
         rc = lib().w4a8_cache_attention(c, b, *q_rows, H, float(scale), max_len, *_token_rows(out, "out"), wk_ptr, wk_bytes,
                                         s.cuda_stream)
-    _check(rc, "w4a8_cache_attention")
+        _check(rc, "w4a8_cache_attention")
     return out

@@ -202,3 +202,72 @@ def test_refused_calls_leave_the_workspace_alone():
         with pytest.raises((TypeError, ValueError)):
             w.w4a8_linear(a["x"], a["wp"], a["sd"], N, out=a["out"], workspace=ws)
         assert ws.buf.numel() == 0, list(bad)
+
+
+def cache_step(B=3, L=3000, H=8, Hkv=2):
+    """A cache of random codes, and a batch of one new token for each sequence."""
+    g = torch.Generator(device=dev()).manual_seed(914)
+    blocks = -(-L // w.CACHE_BLOCK)
+    cache = w.KVCache.empty(B * blocks, B, Hkv, device=dev())
+    for t in cache[:2]:
+        t.copy_(torch.randint(-127, 128, t.shape, generator=g, device=dev()))
+    cache.scales.fill_(0.01)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device=dev())  # noqa: E731
+    table = torch.arange(B * blocks, dtype=torch.int32, device=dev()).view(B, blocks)
+    qkv = torch.randn(B, H + 2 * Hkv, 128, generator=g, device=dev()).to(torch.bfloat16)
+    ang = torch.rand(8, 64, generator=g, device=dev())
+    batch = (i32(*range(B + 1)), i32(*[L] * B), table, i32(*range(B)), ang.cos(), ang.sin())
+    assert w.w4a8_cache_attention_workspace_bytes(B, B, H, Hkv, blocks * 64) > 0
+    return qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:], cache, batch
+
+
+@pytest.mark.parametrize("held", [0, 128])
+@pytest.mark.parametrize("native", [True, False])
+def test_refused_attention_leaves_the_workspace_alone(held, native):
+    q, _, _, cache, batch = cache_step()
+    kw = {} if native else dict(stream=torch.cuda.current_stream())
+    ws = w.Workspace()
+    if held:
+        ws.get(held)
+    buf, home = ws.buf, ws._home
+    odd = torch.zeros(q.numel() + 4, dtype=torch.bfloat16, device=dev())[4:].view(q.shape)  # not 16-byte aligned
+    flat = torch.zeros(1, 8, 128, dtype=torch.bfloat16, device=dev()).expand(3, 8, 128)
+    for bad in (dict(max_len=0), dict(max_len=1 << 20), dict(q=odd), dict(scale=float("nan")), dict(scale=float("inf")), dict(out=odd),
+                dict(out=flat), dict(cos=torch.zeros(8 * 64 + 2, device=dev())[2:].view(8, 64))):
+        a = dict(q=q, scale=0.1, max_len=None, out=None, cos=batch[4]) | bad
+        with pytest.raises(w.W4A8Error):
+            w.w4a8_cache_attention(a["q"], cache, *batch[:4], a["cos"], batch[5], a["scale"], max_len=a["max_len"], out=a["out"],
+                                   workspace=ws, **kw)
+        assert ws.buf is buf and ws._home is home, list(bad)
+    y = w.w4a8_cache_attention(q, cache, *batch, 0.1, workspace=ws, **kw)
+    assert ws.buf.numel() > held
+    same(y, w.w4a8_cache_attention(q, cache, *batch, 0.1))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_calls_that_the_library_refuses_leave_the_workspace_alone(native):
+    kw = {} if native else dict(stream=torch.cuda.current_stream())
+    K, N, M = 512, 64, 20
+    x = bf16_dev(I.activations(M, K, 918))
+    W, s = I.weights(N, K, 919)
+    wp, sd = pack(W), scales_dev(s)
+    shifted = lambda t: torch.cat([t.new_zeros(4), t.flatten()])[4:].view(t.shape)  # noqa: E731  (not 16-byte aligned)
+    ws = w.Workspace()
+    buf, home = ws.buf, ws._home
+    for f in (w.w4a8_linear, w.w4a8_linear_swiglu):
+        for bad in (dict(x=shifted(x)), dict(wp=shifted(wp))):
+            a = dict(x=x, wp=wp) | bad
+            with pytest.raises(w.W4A8Error):
+                f(a["x"], a["wp"], sd, N, workspace=ws, **kw)
+            assert ws.buf is buf and ws._home is home, list(bad)
+    q = bf16_dev(I.activations(2 * 5, 128, 920)).view(2, 5, 128)
+    i = torch.arange(5, dtype=torch.int32, device=dev())
+    t = torch.ones(5, 64, device=dev())
+    for bad in (dict(q=shifted(q)), dict(scale=float("nan"))):
+        a = dict(q=q, scale=0.1) | bad
+        with pytest.raises(w.W4A8Error):
+            w.w4a8_stream_attention(a["q"], q, q, i, i, t, t, a["scale"], workspace=ws, **kw)
+        assert ws.buf is buf and ws._home is home, list(bad)
+    y = w.w4a8_linear(x, wp, sd, N, workspace=ws, **kw)
+    assert ws.buf.numel() > 0
+    same(y, w.w4a8_linear(x, wp, sd, N))
