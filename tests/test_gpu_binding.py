@@ -221,6 +221,84 @@ def cache_step(B=3, L=3000, H=8, Hkv=2):
     return qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:], cache, batch
 
 
+def test_native_path_is_taken_by_the_cache_calls(monkeypatch):
+    rec = Record(monkeypatch)
+    cur = torch.cuda.current_stream()
+    K, M = 512, 20
+    x, r = (bf16_dev(I.activations(M, K, s)) for s in (915, 916))
+    gain = torch.linspace(0.5, 1.5, K, device=dev()).to(torch.bfloat16)
+    ref = w.w4a8_add_rmsnorm_quantize_act(x, r, gain, 1e-6, stream=cur)
+    for out in (None, torch.empty_like(x)):
+        y, got = rec.last(w.w4a8_add_rmsnorm_quantize_act, x, r, gain, 1e-6, out=out)
+        assert y is got and (out is None or y[2] is out)
+        for a, b in zip(y, ref):
+            same(a, b)
+
+    q, k, v, cache, batch = cache_step()
+    twin = w.KVCache(*(t.clone() for t in cache))
+    w.w4a8_cache_append(k, v, twin, *batch, stream=cur)
+    assert rec.last(w.w4a8_cache_append, k, v, cache, *batch) == (None, True)
+    for a, b in zip(cache, twin):
+        same(a, b)
+    slots = torch.arange(3, dtype=torch.int32, device=dev())
+    assert rec.last(w.w4a8_cache_append, k, v, cache, *batch, slots=slots) == (None, True)
+
+    ref = w.w4a8_cache_attention(q, cache, *batch, 0.1, stream=cur)
+    need = w.w4a8_cache_attention_workspace_bytes(3, 3, 8, 2, batch[2].shape[1] * 64)
+    ws = w.Workspace()
+    for wk in (ws, ws, None, torch.zeros(need, dtype=torch.uint8, device=dev())):
+        for out in (None, torch.empty_like(ref), torch.empty(8, 3, 128, dtype=torch.bfloat16, device=dev()).transpose(0, 1)):
+            y, got = rec.last(w.w4a8_cache_attention, q, cache, *batch, 0.1, workspace=wk, out=out)
+            assert y is got and (out is None or y is out)
+            same(y, ref)
+    y, got = rec.last(w.w4a8_cache_attention, q, cache, *batch, 0.1, max_len=3000, workspace=ws)
+    assert y is got
+    bare = w.KVCache(*cache[:3])  # rings are the append's alone
+    y, got = rec.last(w.w4a8_cache_attention, q, bare, *batch, 0.1, workspace=ws)
+    assert y is got
+    same(y, ref)
+
+
+def test_native_path_declines_cache_calls(monkeypatch):
+    import copy
+    rec = Record(monkeypatch)
+    q, k, v, cache, batch = cache_step()
+    ws = w.Workspace()
+    ref = w.w4a8_cache_attention(q, cache, *batch, 0.1, workspace=ws)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):  # a Workspace of another stream, a copy of one
+        y, got = rec.last(w.w4a8_cache_attention, q, cache, *batch, 0.1, workspace=ws)
+        twin = copy.deepcopy(ws)
+    assert got is None
+    side.synchronize()
+    same(y, ref)
+    y, got = rec.last(w.w4a8_cache_attention, q, cache, *batch, 0.1, workspace=twin)
+    assert got is None
+    same(y, ref)
+    y, got = rec.last(w.w4a8_cache_attention, q, cache, *batch, 1, workspace=ws)  # a scale that is no float
+    assert got is None and torch.isfinite(y).all()
+
+    class Sub(torch.Tensor):
+        pass
+
+    y, got = rec.last(w.w4a8_cache_attention, q.as_subclass(Sub), cache, *batch, 0.1, workspace=ws)
+    assert got is None
+    same(y.as_subclass(torch.Tensor), ref)
+    rings = [t.clone() for t in cache]
+    r, got = rec.last(w.w4a8_cache_append, k.as_subclass(Sub), v, cache, *batch)
+    assert r is None and got is None
+    w.w4a8_cache_append(k, v, w.KVCache(*rings), *batch)
+    for a, b in zip(cache, rings):
+        same(a, b)
+    x = bf16_dev(I.activations(4, 256, 917))
+    gain = torch.ones(256, dtype=torch.bfloat16, device=dev())
+    y, got = rec.last(w.w4a8_add_rmsnorm_quantize_act, x.as_subclass(Sub), x, gain, 1e-6)
+    assert got is None
+    for a, b in zip(y, w.w4a8_add_rmsnorm_quantize_act(x, x, gain, 1e-6)):
+        same(a.as_subclass(torch.Tensor), b)
+
+
 @pytest.mark.parametrize("held", [0, 128])
 @pytest.mark.parametrize("native", [True, False])
 def test_refused_attention_leaves_the_workspace_alone(held, native):

@@ -322,6 +322,24 @@ def test_mixed_batch():
         assert (out[sum(new):] == 3.0).all() and not (out[:sum(new)] == 3.0).all(-1).any()
 
 
+@pytest.mark.parametrize("behind", [0, 4])
+def test_output_with_and_without_rows_behind(behind):
+    m = Model(2, 6, 700, seed=31)
+    new = [130, 1, 16, 0, 1, 5]
+    m.append([300, 700, 77, 40, 1, 64])
+    q = bf16_dev(m.values(sum(new) + behind, 8))
+    want = m.attend(q[:sum(new)], new)
+    out = torch.full((sum(new) + behind, 8, D), 3.0, dtype=torch.bfloat16, device=dev())
+    assert m.attend(q, new, behind=behind, out=out) is out
+    # (the number of rows takes part in the choice of the form and splits, so the sums' order may differ by it)
+    o64, tol = m.expect(to_np_bits(q)[:sum(new)], new)
+    for o in (want, out[:sum(new)]):
+        assert (np.abs(o.float().cpu().numpy() - o64) <= tol).all()
+    assert (out[sum(new):] == 3.0).all()
+    if not behind:
+        assert torch.equal(out, want)
+
+
 def test_many_sequences():
     B = 130
     m = Model(1, B, 100, seed=32)
@@ -533,6 +551,26 @@ def test_queries_that_are_no_numbers(n, what):
     hit = torch.zeros(2 * n, 8, dtype=torch.bool, device=dev())
     hit[n - 1, 5] = hit[n, 0] = True
     assert o[hit].isnan().all() and torch.equal(o[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("n", [1, 16, 150])
+def test_rows_beside_large_ones(n):
+    # queries with large scores, and a block with values out of the usual range that only the last rows see, leave the
+    # other rows' results as they are
+    m = Model(2, 2, 400, seed=62)
+    m.append([300, 192 + n])
+    q = bf16_dev(m.values(2 * n, 8))
+    want = m.attend(q, [n, n]).clone()
+    large = q.clone()
+    large[n - 1, 5] *= 2.0 ** 40
+    large[n, 0] *= -(2.0 ** 40)
+    m.cache.scales[int(m.table[1, (191 + n) // BLK]), :, 1] *= 2.0 ** 60
+    o = m.attend(large, [n, n])
+    hit = torch.zeros(2 * n, 8, dtype=torch.bool, device=dev())
+    hit[n - 1, 5] = hit[n, 0] = True
+    last = ((191 + n) // BLK) * BLK - 192  # sequence 1's new tokens from here on see its last block
+    hit[n + max(last, 0):] = True
+    assert torch.equal(o[~hit], want[~hit]) and o.isfinite().all()
 
 
 def test_pages_out_of_range_are_not_seen():
