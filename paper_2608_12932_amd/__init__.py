@@ -371,6 +371,21 @@ def _workspace_ptr(workspace, need: int, device, stream):
     return _dev(buf, "workspace", torch.uint8), buf.numel()
 
 
+def _check_workspace_device(workspace, device) -> None:
+    """A workspace lies on the device of the call.  (That of an empty Workspace
+    of no particular device is settled when it grows.)"""
+    if isinstance(workspace, Workspace):
+        on = workspace.buf.device if workspace.buf.numel() else workspace.device
+        if on.index is None:
+            return
+    elif not getattr(workspace, "is_cuda", False):  # none, or an error of its own
+        return
+    else:
+        on = workspace.device
+    if on != device:
+        raise ValueError(f"workspace is on {on}, the call's tensors on {device}")
+
+
 @contextlib.contextmanager
 def _unless_refused(workspace):
     """A Workspace that grows inside is as it was again where the call is
@@ -698,6 +713,7 @@ def w4a8_cache_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, 
         if out is None:
             out = torch.empty((T, H, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
         need = w4a8_cache_attention_workspace_bytes(b.B, T, H, Hkv, max_len)
+        _check_workspace_device(workspace, q.device)
         wk_ptr, wk_bytes = _workspace_ptr(workspace, need, q.device, s)
         rc = lib().w4a8_cache_attention(c, b, *q_rows, H, float(scale), max_len, *_token_rows(out, "out"), wk_ptr, wk_bytes,
                                         s.cuda_stream)

@@ -131,6 +131,29 @@ def test_binding_checks_before_the_device():
         w.w4a8_cache_attention(x.view(1, 8, 128), c, torch.zeros(2, dtype=torch.int32), i, i[None], i, t, t, 0.1)
 
 
+def test_workspace_of_another_device():
+    class Buffer:  # what the check sees of a device tensor
+        is_cuda = True
+
+        def __init__(self, index, n=8):
+            self.device, self.n = torch.device("cuda", index), n
+
+        def numel(self):
+            return self.n
+
+    def workspace(device, buf):
+        ws = w.Workspace.__new__(w.Workspace)
+        ws.device, ws.buf = torch.device(device), buf
+        return ws
+
+    here = torch.device("cuda", 1)
+    for ok in (None, Buffer(1), workspace("cuda", Buffer(0, 0)), workspace("cuda", Buffer(1)), workspace("cuda:1", Buffer(1, 0))):
+        w._check_workspace_device(ok, here)
+    for bad in (Buffer(0), workspace("cuda", Buffer(0)), workspace("cuda:0", Buffer(0, 0)), workspace("cuda:0", Buffer(0))):
+        with pytest.raises(ValueError):
+            w._check_workspace_device(bad, here)
+
+
 # ---- the oracle
 
 
