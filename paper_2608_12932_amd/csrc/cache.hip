@@ -313,6 +313,13 @@ __device__ __forceinline__ uint4 output8(const float (&o)[8], float total) {
   return make_uint4(two(0), two(2), two(4), two(6));
 }
 
+// A total moved by the factor 2^d, d <= 0: by one product, or, where that would
+// vanish while the total (which may be as large as 2^127) does not, by two.
+__device__ __forceinline__ float rescaled(float total, float d) {
+  const float half = __builtin_amdgcn_exp2f(0.5f * d);
+  return d < -kFar ? total * half * half : total * __builtin_amdgcn_exp2f(d);
+}
+
 // The larger (sum) of the values of lanes l, l ^ 16, l ^ 32 and l ^ 48.
 template <class F>
 __device__ __forceinline__ float fold_groups(float x, F op) {
@@ -677,39 +684,39 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
       top[t] = fold_groups(fmaf(top[t], f[t], vl[t]), [](float p, float r) { return fmaxf(p, r); });
       outgrown = outgrown || top[t] - m[t] > kSlack;
     }
-    if (__builtin_expect(careful || __any(outgrown), 0)) {
+    if (__any(outgrown)) {
+      bool large = false;
 #pragma unroll
       for (int t = 0; t < R; ++t) {
         // a row's own maximum alone moves its offset: its result does not
         // depend on the rows that share the wave
         const bool up = top[t] - m[t] > kSlack;
-        // in two steps: where the values' scales jump the total stays in
-        // range, and the factor would not
-        const float half = up ? __builtin_amdgcn_exp2f(0.5f * (m[t] - top[t])) : 1.0f, alpha = half * half;
+        l[t] = rescaled(l[t], up ? m[t] - top[t] : 0.0f);
+        const float alpha = up ? __builtin_amdgcn_exp2f(m[t] - top[t]) : 1.0f;
         m[t] = up ? top[t] : m[t];
-        l[t] = l[t] * half * half;
+        large = large || (fabsf(m[t]) >= kLarge && m[t] != -INFINITY);
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
-        const bool large = fabsf(m[t]) >= kLarge && m[t] != -INFINITY;
-        careful = careful || __any(large);
-        if (__builtin_expect(careful, 0)) {
-          wild[t] = wild[t] || (top[t] > -INFINITY && !(vlog >= kLowLog2 && vlog <= kHighLog2));
-          const bool apart = large || (wild[t] && top[t] < m[t] - kFar);
-          const float shift = m[t] + kWeightShift - m[t];  // what the offset below becomes: 12, and m's rounding
-          float sum = 0.0f;
+      }
+      careful = careful || __any(large);
+    }
+    if (__builtin_expect(careful, 0)) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float y = fmaf(x[t][e], f[t], vl[t]) - m[t];
-            sum += __builtin_amdgcn_exp2f(y - vl[t] + kTotalShift);
-            x[t][e] = apart ? y + (kWeightShift - shift) : x[t][e];
-          }
-          if (apart) {
-            l[t] += sum;
-            f[t] = 1.0f;
-            vl[t] = m[t];
-            vi[t] = 0.0f;
-          }
+      for (int t = 0; t < R; ++t) {
+        wild[t] = wild[t] || (top[t] > -INFINITY && !(vlog >= kLowLog2 && vlog <= kHighLog2));
+        const bool apart = (fabsf(m[t]) >= kLarge && m[t] != -INFINITY) || (wild[t] && top[t] < m[t] - kFar);
+        const float shift = m[t] + kWeightShift - m[t];  // what the offset below becomes: 12, and m's rounding
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float y = fmaf(x[t][e], f[t], vl[t]) - m[t];
+          sum += __builtin_amdgcn_exp2f(y - vl[t] + kTotalShift);
+          x[t][e] = apart ? y + (kWeightShift - shift) : x[t][e];
         }
+        l[t] += apart ? sum : 0.0f;
+        f[t] = apart ? 1.0f : f[t];
+        vl[t] = apart ? m[t] : vl[t];
+        vi[t] = apart ? 0.0f : vi[t];
       }
     }
 
@@ -805,8 +812,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const float2 ml = l_ml[r + w * kRows];
-        const float half = __builtin_amdgcn_exp2f(0.5f * (ml.x - base)), f = half * half;  // as above
-        lsum = fmaf(ml.y * half, half, lsum);
+        const float f = __builtin_amdgcn_exp2f(ml.x - base);
+        lsum += rescaled(ml.y, ml.x - base);
         const float* p = &l_o[(r + w * kRows) * kPitch + d];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(p[e], f, o[e]);
@@ -859,10 +866,8 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
     Partial r;
     r.mx = fmaxf(x.mx, y.mx);
     const float base = r.mx == -INFINITY ? 0.0f : r.mx;
-    // in two steps, as the attention moves its offset
-    const float h0 = __builtin_amdgcn_exp2f(0.5f * (x.mx - base)), h1 = __builtin_amdgcn_exp2f(0.5f * (y.mx - base));
-    const float f0 = h0 * h0, f1 = h1 * h1;
-    r.sum = x.sum * h0 * h0 + y.sum * h1 * h1;
+    const float f0 = __builtin_amdgcn_exp2f(x.mx - base), f1 = __builtin_amdgcn_exp2f(y.mx - base);
+    r.sum = rescaled(x.sum, x.mx - base) + rescaled(y.sum, y.mx - base);
 #pragma unroll
     for (int e = 0; e < 8; ++e) r.o[e] = x.o[e] * f0 + y.o[e] * f1;
     return r;
