@@ -126,11 +126,11 @@ constexpr int kCodePitch = kD + 4;                  // bytes of a token's codes 
 // there the workgroup of fb, once it has read them, writes the ring for the
 // block that takes their place.
 //
-// Bound by its chain of reads, each of which waits for the one before (the
-// batch; positions, slot and page; rows and tables), not by bytes: 5.5 us for
-// 16 sequences' single tokens at 8 kv heads, 6.6 us for 1024 tokens (6.8 MB, 1.3 us
-// at a copy's rate); with 256 threads in two passes and the page read last 6.0
-// and 6.8.
+// Bound by its chain of reads, each of which waits for the one before, not by
+// bytes: the batch, the slot, rows and positions, the tables, and (the compiler
+// puts it right before the barrier) the page.  5.3 us for 16 sequences' single
+// tokens at 8 kv heads, 6.7 us for 1024 tokens (6.8 MB, 1.3 us at a copy's
+// rate); with 256 threads in two passes 6.0 and 6.8.
 __global__ __launch_bounds__(kAppendThreads) void cache_append(const CacheAppendArgs a) {
   __shared__ uint32_t l_max[kAppendThreads / 64];
   __shared__ uint8_t l_codes[kBlock * kCodePitch];
@@ -144,15 +144,14 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append(const CacheAppend
   const int first = max(s.len - s.n, 0);  // the first new token that has a place
   const int fb = first / kBlock, last = (s.len - 1) / kBlock, blk = fb + s.item;
   const int slot = a.slots ? a.slots[s.b] : s.b;
-  const int page = cb.table[(int64_t)s.b * cb.max_blocks + blk];  // needed last: nothing waits for it
+  const int page = cb.table[(int64_t)s.b * cb.max_blocks + blk];
   const bool slot_ok = slot >= 0 && slot < a.n_slots;
   const TokenRows rows = keys ? a.k : a.v;
   uint16_t* ring = (keys ? a.k_recent : a.v_recent) + ((int64_t)(slot_ok ? slot : 0) * cb.Hkv + hk) * (kRecent * kD);
   const int c = tid & 7;
 
-  // Chunks c and c + 8 of token t: rotated if it is a new key.  Every lane
-  // loads, one without a token the call's last one, so that nothing waits for
-  // a branch.
+  // Chunks c and c + 8 of token t: rotated if it is a new key.  A lane without
+  // a token loads the call's last one.
   auto load = [&](int t, uint4& lo, uint4& hi) {
     const bool held = t < first, there = t < s.len && (!held || slot_ok);
     const int row = s.row0 + (there && !held ? t - (s.len - s.n) : s.n - 1);
@@ -700,6 +699,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
       }
       careful = careful || __any(large);
     }
+    // Rows with a large offset, and rows far above a block after a scale out of
+    // the range (kFar): the weights from the rounded score less the offset, the
+    // total from the scores alone.  That the loop has this way at all costs 1 - 2 %
+    // of a call (1024 over 8192: 150 us without it, 153 with it).
     if (__builtin_expect(careful, 0)) {
 #pragma unroll
       for (int t = 0; t < R; ++t) {
@@ -861,7 +864,7 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
   const int tid = threadIdx.x, c = tid % kChunks, part = tid / kChunks % P;
   const int64_t row = (int64_t)blockIdx.x * kRowsHere + tid / (kChunks * P), rows = (int64_t)a.c.T * a.H;
   const int64_t tok = row / a.H;
-  const int first = a.c.starts[0], end = a.c.starts[a.c.B];  // needed last: nothing waits for them
+  const int first = a.c.starts[0], end = a.c.starts[a.c.B];
   auto fold = [](const Partial& x, const Partial& y) {
     Partial r;
     r.mx = fmaxf(x.mx, y.mx);
@@ -926,6 +929,12 @@ __global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs
 // 1 %.  us of 16 / 64 / 128 rows, at its best splits each: 8 x 16 tokens over
 // 2500 20.4 23.2 27.6, 23 x 27 over 478 30.5 20.8 19.1, 1024 over 8192 326 195
 // 155.
+//   The calls were of one kind of sequence each.  A batch is taken as B
+// sequences of max_len with the average number of new tokens, so one that mixes
+// kinds gets the form and splits of neither.  us of the batch, and of its two
+// parts as calls of their own: one token over 100000 among 63 over 200 673, 41 +
+// 10; a chunk of 1024 among 8 single tokens, all over 8192, 249, 153 + 27; among
+// 32 343, 153 + 83; a chunk of 193 among 63 251, 53 + 160.
 typedef void (*AttnFn)(const CacheAttnArgs);
 struct AttnForm {
   int rows, KW, threads;
@@ -937,10 +946,11 @@ const AttnForm kForms[] = {
     {64, 1, 256, 1570, 1010, 1840, 720, cache_attention<1, 1, 4>},
     {128, 2, 512, 3010, 50, 8830, 1600, cache_attention<2, 2, 8>},
 };
-// A cache that is read once and is larger than this does not stay in the
-// memory-side cache (256 MB) until the next call: it is read past it.  us with /
-// without: 64 sequences of 4096 (537 MB) 84 / 99, one of 100000 (205 MB) 39 / 44;
-// of 131 MB, when called again and again, 28.4 / 27.7.
+// A cache that is read once (by the average of new tokens, as above) and is
+// larger than this does not stay in the memory-side cache (256 MB) until the
+// next call: it is read past it.  us with / without: 64 sequences of 4096 (537 MB)
+// 84 / 99, one of 100000 (205 MB) 39 / 44; of 131 MB, when called again and again,
+// 28.4 / 27.7.
 constexpr int64_t kStreamBytes = int64_t(160) << 20;
 const AttnFn kStreamFn = cache_attention<1, 4, 4, kCacheStream>;
 constexpr int64_t kMaxAxis = 65535;  // workgroups along the second and third axis of a launch
