@@ -655,7 +655,9 @@ def w4a8_cache_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, starts: 
     batch: int32 starts [B + 1] (rows starts[b] .. are sequence b's new
     tokens), lengths [B] (tokens held, the new ones included), table
     [B][blocks] (pages), pos [T]; fp32 rotary tables [n_pos][64]; slots int32
-    [B], the ring of each sequence (None: sequence b has ring b)."""
+    [B], the ring of each sequence (None: sequence b has ring b); one out of
+    range is none, and the append leaves a block that was started before as
+    it is."""
     if stream is None:
         r = (_fast or _load_fast()).cache_append(k, v, cache, starts, lengths, table, pos, rope_cos, rope_sin, slots)
         if r is not None:
