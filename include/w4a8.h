@@ -354,6 +354,143 @@ w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batc
 size_t w4a8_cache_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hkv, int64_t max_len);
 
 /*
+ * RMSNorm of each query and key head and its rotation, in one pass over the
+ * fused QKV projection's output: what a decoder layer with head norms does
+ * between that projection and its cache or attention.  For each token t and
+ * head x of 128 elements
+ *     r = 1 / sqrt(sum_d x_d^2 / 128 + eps),  h_d = (x_d r) gamma_d
+ *     y_d = h_d cos_i - h_{d+64} sin_i,  y_{d+64} = h_{d+64} cos_i + h_d sin_i
+ * for the pairs i = d < 64, with cos_i = rope_cos[p][i], sin_i = rope_sin[p][i]
+ * and p = pos[axis[i]][t]: positions may have several axes (time, height and
+ * width of an image's or video's tokens), each of which turns its own pairs.
+ * fp32 throughout, rounded once, to bf16.  The mean square has to be finite in
+ * fp32.
+ *   x, out       device, bf16, 16-byte aligned: token t, head h at t * row + h *
+ *                head elements (out: out_row, out_head), 128 in a row; strides
+ *                in multiples of 8.  out is x itself with x's strides (in
+ *                place), or apart from both kinds' inputs and from the other's
+ *                output (W4A8_EINVAL where that cannot be seen from two equal
+ *                strides or disjoint ranges); its rows must not overlap each
+ *                other, nor any other argument
+ *   heads        0 .. 4096 (0: none of this kind, its pointers are not read)
+ *   gamma        device, bf16 gain [128], 16-byte aligned, or NULL: no norm
+ *   eps          0 < eps < inf
+ *   rope         NULL: no rotation.  pos: device, int32 [n_axes][T], clamped to
+ *                [0, n_pos); n_axes 1 .. 4; axis: host, the axis of each of the
+ *                64 pairs, read by the call, or NULL: axis 0; tables device,
+ *                fp32 [n_pos][64], 16-byte aligned, n_pos 1 .. 2^30
+ *   q, k         either may be NULL (no heads of this kind)
+ *   T            0 <= T <= W4A8_M_MAX (0: a no-op)
+ * A call without a norm and without a rotation is W4A8_EINVAL.  Does not
+ * synchronize; enqueues one kernel; deterministic.
+ */
+typedef struct {
+  const uint16_t* x;
+  int64_t row, head, heads;
+  const uint16_t* gamma;
+  uint16_t* out;
+  int64_t out_row, out_head;
+} w4a8_heads;
+typedef struct {
+  const int32_t* pos;
+  int64_t n_axes;
+  const uint8_t* axis;
+  const float* rope_cos;
+  const float* rope_sin;
+  int64_t n_pos;
+} w4a8_rope;
+w4a8_status w4a8_qk_norm_rope(const w4a8_heads* q, const w4a8_heads* k, int64_t T, float eps, const w4a8_rope* rope,
+                              hipStream_t stream);
+
+/*
+ * The 4-bit key/value cache: 9/16 of the bytes of the 8-bit one.  Blocks, pages
+ * and tables are as there, but every token is held by itself: its keys (as they
+ * are given: rotate them first, w4a8_qk_norm_rope) and values of a kv head, each
+ * in two groups of 64 elements with a scale s and an offset b in fp16,
+ *     s = fp16((hi - lo) / 15),  b = fp16(lo - 16 s),
+ *     code = min(max(round_half_even((x - b) / s - 16), 0), 15)  (0 where s = 0),
+ * fp32 IEEE operations, with lo and hi the group's least and largest; the code
+ * stands for fp16(s (16 + code) + b), rounded once.  Magnitudes above 2^14 count
+ * as 2^14, NaN as 0, so that scales and offsets are finite whatever comes in; a
+ * group whose elements lie within 15 * 2^-25 of each other is held as lo.
+ *   A token's codes depend on the token alone: there is no ring, tokens can be
+ * taken back by appending again after any smaller length, and an append leaves
+ * every other token's codes as they are.
+ *   A word of eight codes holds element 2 i in bits 4 i .. and element 2 i + 1 in
+ * bits 16 + 4 i .. (i < 4).
+ *   k_codes      device, uint32 [n_pages][Hkv][4][16][16], 16-byte aligned: token
+ *                4 i + j of the block in [j][i], a word of its 8 elements 8 w ..
+ *                in [w]
+ *   v_codes      device, uint32 [n_pages][Hkv][8][2][16][4], 16-byte aligned:
+ *                tokens 8 t .. of the block at d = 8 i + 4 j + l in the word
+ *                [t][j][i][l]
+ *   k_params     device, fp16 [n_pages][Hkv][2][64][2], 16-byte aligned: group,
+ *                token, scale and offset
+ *   v_params     device, fp16 [n_pages][Hkv][2][2][64], 16-byte aligned: group,
+ *                scales and offsets, token
+ */
+typedef struct {
+  uint32_t* k_codes;
+  uint32_t* v_codes;
+  uint16_t* k_params;
+  uint16_t* v_params;
+  int64_t n_pages, Hkv;
+} w4a8_cache4;
+
+/*
+ * Appends the batch's new keys and values.  The batch is that of the 8-bit
+ * cache's calls, without positions and tables: pos, rope_cos, rope_sin and
+ * n_pos are not read.
+ *   k, v         device, bf16, 16-byte aligned: token t, kv head h at t * k_row
+ *                + h * k_head elements, 128 in a row; strides in multiples of 8
+ * Every sequence of a call needs pages of its own where it writes.  Tokens whose
+ * page is outside [0, n_pages) are not held.  Hkv <= 4096, n_pages below 2^31.
+ * Does not synchronize; enqueues one kernel; deterministic.
+ */
+w4a8_status w4a8_cache4_append(const w4a8_cache4* cache, const w4a8_batch* batch, const uint16_t* k, int64_t k_row,
+                               int64_t k_head, const uint16_t* v, int64_t v_row, int64_t v_head, hipStream_t stream);
+
+/*
+ * Reads tokens back: rows starts[b] .. starts[b + 1] - 1 of the outputs receive
+ * the last starts[b + 1] - starts[b] of the lengths[b] tokens that sequence b
+ * holds (the rows that appended them; all of them where the starts are the sums
+ * of the lengths), as the values that the codes stand for, rounded to bf16.
+ * Rows of tokens without a page are zeros; rows of no sequence, and rows before
+ * a sequence's first token, are left as they are.
+ *   k, v         device, bf16, 16-byte aligned: token t, kv head h at t * k_row
+ *                + h * k_head elements; strides in multiples of 8.  Either may be
+ *                NULL (not read back).  Rows must not overlap each other, the
+ *                other output (as in w4a8_qk_norm_rope) or the cache
+ * With head strides above the row strides the output is [Hkv][tokens][128], as
+ * w4a8_stream_attention takes it.  Does not synchronize; enqueues one kernel.
+ */
+w4a8_status w4a8_cache4_read(const w4a8_cache4* cache, const w4a8_batch* batch, uint16_t* k, int64_t k_row, int64_t k_head,
+                             uint16_t* v, int64_t v_row, int64_t v_head, hipStream_t stream);
+
+/*
+ * w4a8_cache_attention over the 4-bit cache: for each query head h and new
+ * token i of a sequence with n new tokens and length L,
+ *     o[i][h] = sum_j softmax_j(scale * q[i][h] . k[j]) v[j]
+ * over its tokens j <= L - n + i; q as it is given (rotate it first).  A token
+ * that sees nothing gets 0.
+ *   A query is held in fp16 at its own power of two (elements down to 2^-28 of
+ * its largest exactly), its products with the keys' fp16 values are summed in
+ * fp32; softmax and sums run in fp32, the softmax weights are rounded to fp16
+ * for the product with the values (2^-11 relative; one below 2^-26 of the row's
+ * largest, to 2^-37 of that); the output is rounded to bf16.  Scores, and scale
+ * times any element of a query, have to lie within fp32's range.
+ *   Arguments as for w4a8_cache_attention, the batch as for w4a8_cache4_append;
+ * the workspace has its own size query below.
+ */
+w4a8_status w4a8_cache4_attention(const w4a8_cache4* cache, const w4a8_batch* batch, const uint16_t* q, int64_t q_row,
+                                  int64_t q_head, int64_t H, float scale, int64_t max_len, uint16_t* o, int64_t o_row,
+                                  int64_t o_head, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes w4a8_cache4_attention needs (0 if none, and 0 for shapes it
+ * rejects). */
+size_t w4a8_cache4_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hkv, int64_t max_len);
+
+/*
  * Bytes of device workspace w4a8_linear needs for this problem (0 if none).
  * The workspace holds split-K partial sums and arrival counters (and, when
  * bf16 input is quantized by its own kernel, the int8 codes and scales).

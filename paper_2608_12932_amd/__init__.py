@@ -33,7 +33,9 @@ EXPORTS = ("w4a8_status_string", "w4a8_packed_weight_bytes", "w4a8_pack_weights"
            "w4a8_linear_swiglu_describe", "w4a8_rmsnorm_quantize_act", "w4a8_stream_attention",
            "w4a8_stream_attention_workspace_bytes", "w4a8_flow_schedule", "w4a8_flow_step",
            "w4a8_linear_noalloc", "w4a8_add_rmsnorm_quantize_act", "w4a8_cache_append",
-           "w4a8_cache_attention", "w4a8_cache_attention_workspace_bytes")
+           "w4a8_cache_attention", "w4a8_cache_attention_workspace_bytes", "w4a8_qk_norm_rope",
+           "w4a8_cache4_append", "w4a8_cache4_read", "w4a8_cache4_attention",
+           "w4a8_cache4_attention_workspace_bytes")
 CACHE_BLOCK, CACHE_RECENT, HEAD_DIM = 64, 128, 128
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
@@ -50,6 +52,21 @@ class _BatchArgs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("starts", "lengths", "table")] + [
         (n, ctypes.c_int64) for n in ("max_blocks", "B", "T")] + [
         (n, ctypes.c_void_p) for n in ("pos", "rope_cos", "rope_sin")] + [("n_pos", ctypes.c_int64)]
+
+
+class _Cache4Args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_params", "v_params")] + [
+        ("n_pages", ctypes.c_int64), ("Hkv", ctypes.c_int64)]
+
+
+class _HeadsArgs(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64), ("heads", ctypes.c_int64),
+                ("gamma", ctypes.c_void_p), ("out", ctypes.c_void_p), ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64)]
+
+
+class _RopeArgs(ctypes.Structure):
+    _fields_ = [("pos", ctypes.c_void_p), ("n_axes", ctypes.c_int64), ("axis", ctypes.c_char_p), ("rope_cos", ctypes.c_void_p),
+                ("rope_sin", ctypes.c_void_p), ("n_pos", ctypes.c_int64)]
 
 
 class W4A8Error(RuntimeError):
@@ -115,6 +132,18 @@ def lib() -> ctypes.CDLL:
         L.w4a8_cache_attention.restype = I
         L.w4a8_cache_attention_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
         L.w4a8_cache_attention_workspace_bytes.restype = SZ
+        H, R = ctypes.POINTER(_HeadsArgs), ctypes.POINTER(_RopeArgs)
+        L.w4a8_qk_norm_rope.argtypes = [H, H, I64, ctypes.c_float, R, P]
+        L.w4a8_qk_norm_rope.restype = I
+        C4 = ctypes.POINTER(_Cache4Args)
+        L.w4a8_cache4_append.argtypes = [C4, B, P, I64, I64, P, I64, I64, P]
+        L.w4a8_cache4_append.restype = I
+        L.w4a8_cache4_read.argtypes = [C4, B, P, I64, I64, P, I64, I64, P]
+        L.w4a8_cache4_read.restype = I
+        L.w4a8_cache4_attention.argtypes = [C4, B, P, I64, I64, I64, ctypes.c_float, I64, P, I64, I64, P, SZ, P]
+        L.w4a8_cache4_attention.restype = I
+        L.w4a8_cache4_attention_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
+        L.w4a8_cache4_attention_workspace_bytes.restype = SZ
         L.w4a8_linear_workspace_bytes.argtypes = [I64, I64, I64, I, I]
         L.w4a8_linear_workspace_bytes.restype = SZ
         L.w4a8_linear.argtypes = [P, I, P, I64, I64, P, P, I, I64, P, I, P, SZ, P]
@@ -720,4 +749,217 @@ def w4a8_cache_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, 
         rc = lib().w4a8_cache_attention(c, b, *q_rows, H, float(scale), max_len, *_token_rows(out, "out"), wk_ptr, wk_bytes,
                                         s.cuda_stream)
         _check(rc, "w4a8_cache_attention")
+    return out
+
+
+def rope_axes(sections, interleaved: bool = False) -> bytes:
+    """The axis of each of the 64 rotary pairs (d, d + 64) for w4a8_qk_norm_rope:
+    sections[a] pairs turn by axis a (time, height, width, ..; 64 in all), one
+    axis after the other, or interleaved among A axes: axis a > 0 has the pairs
+    a, a + A, .., axis 0 the others."""
+    sections = [int(n) for n in sections]
+    A, pairs = len(sections), HEAD_DIM // 2
+    if not 1 <= A <= 4 or min(sections) < 0 or sum(sections) != pairs:
+        raise ValueError(f"sections must be 1 to 4 counts that make {pairs}")
+    if not interleaved:
+        return b"".join(bytes([a]) * n for a, n in enumerate(sections))
+    axis = bytearray(pairs)
+    for a in range(1, A):
+        at = range(a, pairs, A)[:sections[a]]
+        if len(at) < sections[a]:
+            raise ValueError(f"axis {a} of {A} interleaved ones has {len(range(a, pairs, A))} pairs at most")
+        for i in at:
+            axis[i] = a
+    return bytes(axis)
+
+
+def _heads_args(x, gamma, out, T, name) -> _HeadsArgs | None:
+    if x is None:
+        return None
+    x_rows = _token_rows(x, name)
+    if x.shape[0] != T:
+        raise ValueError(f"{name} must be [{T}][heads][{HEAD_DIM}]")
+    if out.shape != x.shape:
+        raise ValueError(f"{name}_out must be [{T}][{x.shape[1]}][{HEAD_DIM}]")
+    g = None
+    if gamma is not None:
+        g = _dev(gamma, f"gamma_{name}", torch.bfloat16)
+        if tuple(gamma.shape) != (HEAD_DIM,):
+            raise ValueError(f"gamma_{name} must be [{HEAD_DIM}]")
+    return _HeadsArgs(*x_rows, x.shape[1], g, *_token_rows(out, f"{name}_out"))
+
+
+def w4a8_qk_norm_rope(q: torch.Tensor | None, k: torch.Tensor | None, gamma_q: torch.Tensor | None, gamma_k: torch.Tensor | None,
+                      eps: float, pos: torch.Tensor | None, rope_cos: torch.Tensor | None, rope_sin: torch.Tensor | None,
+                      axes=None, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
+    """RMSNorm (gains bf16 [128], None: no norm) of each head of q bf16
+    [T][H][128] and k bf16 [T][Hkv][128] and their rotation at pos, in one pass
+    -> (q, k) bf16; strided views are allowed, and q_out, k_out take the results,
+    also in place (q_out=q).  q or k may be None.  pos: int32 [T], or [A][T] with
+    the axis (0 .. A - 1) of each of the 64 pairs in `axes` (rope_axes, or any 64
+    numbers); None: no rotation.  fp32 rotary tables [n_pos][64]."""
+    first = q if q is not None else k
+    if first is None:
+        return None, None
+    if axes is not None and type(axes) is not bytes:
+        axes = bytes(axes)
+    if stream is None:
+        r = (_fast or _load_fast()).qk_norm_rope(q, k, gamma_q, gamma_k, eps, pos, rope_cos, rope_sin, axes, q_out, k_out)
+        if r is not None:
+            return r if type(r) is tuple else _check(r, "w4a8_qk_norm_rope")
+    T = first.shape[0]
+    for name, x in (("q", q), ("k", k)):
+        if x is not None:
+            _token_rows(x, name)
+    rope = None
+    if pos is not None:
+        if pos.dim() not in (1, 2) or pos.shape[-1] != T:
+            raise ValueError(f"pos must be [{T}] or [axes][{T}]")
+        if axes is not None and len(axes) != HEAD_DIM // 2:
+            raise ValueError(f"axes must name the axis of each of {HEAD_DIM // 2} pairs")
+        if rope_cos.shape != rope_sin.shape or rope_cos.dim() != 2 or rope_cos.shape[1] != HEAD_DIM // 2:
+            raise ValueError(f"rotary tables must be [n_pos][{HEAD_DIM // 2}]")
+        rope = _RopeArgs(_dev(pos, "pos", torch.int32), pos.shape[0] if pos.dim() == 2 else 1, axes,
+                         _dev(rope_cos, "rope_cos", torch.float32), _dev(rope_sin, "rope_sin", torch.float32), rope_cos.shape[0])
+    with _call_on(stream, first, q=q, k=k, gamma_q=gamma_q, gamma_k=gamma_k, pos=pos, rope_cos=rope_cos, rope_sin=rope_sin,
+                  q_out=q_out, k_out=k_out) as s:
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=k.device)
+        rc = lib().w4a8_qk_norm_rope(_heads_args(q, gamma_q, q_out, T, "q"), _heads_args(k, gamma_k, k_out, T, "k"), T, float(eps),
+                                     rope, s.cuda_stream)
+    _check(rc, "w4a8_qk_norm_rope")
+    return (None if q is None else q_out), (None if k is None else k_out)
+
+
+class KVCache4(NamedTuple):
+    """The tensors of a 4-bit key/value cache, a pool of pages of CACHE_BLOCK
+    tokens: words of eight codes int32 [pages][Hkv][4][16][16] (keys) and
+    [pages][Hkv][8][2][16][4] (values), scales and offsets fp16
+    [pages][Hkv][2][64][2] (keys) and [pages][Hkv][2][2][64] (values); the
+    header says which element lies where.  w4a8_cache4_read gives the values
+    back."""
+
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_params: torch.Tensor
+    v_params: torch.Tensor
+
+    @classmethod
+    def empty(cls, pages: int, Hkv: int, device="cuda") -> "KVCache4":
+        """A zero-filled cache of `pages` pages."""
+        z = lambda dtype, *shape: torch.zeros((pages, Hkv) + shape, dtype=dtype, device=device)  # noqa: E731
+        return cls(z(torch.int32, 4, 16, 16), z(torch.int32, 8, 2, 16, 4), z(torch.float16, 2, CACHE_BLOCK, 2),
+                   z(torch.float16, 2, 2, CACHE_BLOCK))
+
+
+def _cache4_args(cache: KVCache4) -> tuple[_Cache4Args, int]:
+    """The library's view of a 4-bit cache, its shapes checked, and its kv heads."""
+    k = cache.k_codes
+    if k.dim() != 5 or tuple(k.shape[2:]) != (4, 16, 16):
+        raise ValueError("k_codes must be [pages][Hkv][4][16][16]")
+    pages, Hkv = k.shape[:2]
+    for name, shape in (("v_codes", (8, 2, 16, 4)), ("k_params", (2, CACHE_BLOCK, 2)), ("v_params", (2, 2, CACHE_BLOCK))):
+        if tuple(getattr(cache, name).shape) != (pages, Hkv) + shape:
+            raise ValueError(f"{name} must be {''.join(f'[{n}]' for n in (pages, Hkv) + shape)}")
+    i32, f16 = torch.int32, torch.float16
+    return _Cache4Args(_dev(k, "k_codes", i32), _dev(cache.v_codes, "v_codes", i32), _dev(cache.k_params, "k_params", f16),
+                       _dev(cache.v_params, "v_params", f16), pages, Hkv), Hkv
+
+
+def _batch4_args(T, starts, lengths, table) -> _BatchArgs:
+    """The library's view of a batch of T rows without positions, its shapes checked."""
+    B = lengths.shape[0]
+    if lengths.dim() != 1 or tuple(starts.shape) != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("starts, lengths and table must be [B + 1], [B] and [B][blocks]")
+    i32 = torch.int32
+    return _BatchArgs(_dev(starts, "starts", i32), _dev(lengths, "lengths", i32), _dev(table, "table", i32), table.shape[1], B, T,
+                      None, None, None, 0)
+
+
+def w4a8_cache4_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache4, starts: torch.Tensor, lengths: torch.Tensor,
+                       table: torch.Tensor, stream=None) -> None:
+    """Append a step's new keys (rotated already, w4a8_qk_norm_rope) and values
+    to the 4-bit cache, in place.  k, v: bf16 [T][Hkv][128], strided views
+    allowed.  The batch: int32 starts [B + 1] (rows starts[b] .. are sequence b's
+    new tokens), lengths [B] (tokens held, the new ones included), table
+    [B][blocks] (pages)."""
+    if stream is None:
+        r = (_fast or _load_fast()).cache4_append(k, v, cache, starts, lengths, table)
+        if r is not None:
+            return None if r is True else _check(r, "w4a8_cache4_append")
+    k_rows, v_rows = _token_rows(k, "k"), _token_rows(v, "v")
+    c, Hkv = _cache4_args(cache)
+    if k.shape[1] != Hkv or v.shape != k.shape:
+        raise ValueError(f"k and v must be [T][{Hkv}][{HEAD_DIM}]")
+    b = _batch4_args(k.shape[0], starts, lengths, table)
+    with _call_on(stream, k, v=v, starts=starts, lengths=lengths, table=table, **cache._asdict()) as s:
+        rc = lib().w4a8_cache4_append(c, b, *k_rows, *v_rows, s.cuda_stream)
+    _check(rc, "w4a8_cache4_append")
+
+
+def w4a8_cache4_read(cache: KVCache4, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, rows: int,
+                     k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, stream=None):
+    """Tokens of the 4-bit cache back as (k, v) bf16 [rows][Hkv][128]: rows
+    starts[b] .. starts[b + 1] - 1 are the last of the lengths[b] tokens that
+    sequence b holds.  k_out, v_out take the results and may be strided views
+    (also of [Hkv][rows][128], transposed); rows of no sequence are not written."""
+    if stream is None:
+        r = (_fast or _load_fast()).cache4_read(cache, starts, lengths, table, rows, k_out, v_out)
+        if r is not None:
+            return r if type(r) is tuple else _check(r, "w4a8_cache4_read")
+    c, Hkv = _cache4_args(cache)
+    b = _batch4_args(rows, starts, lengths, table)
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is not None and tuple(t.shape) != (rows, Hkv, HEAD_DIM):
+            raise ValueError(f"{name} must be [{rows}][{Hkv}][{HEAD_DIM}]")
+    others = {n: t for n, t in cache._asdict().items() if n != "k_codes"}
+    with _call_on(stream, cache.k_codes, starts=starts, lengths=lengths, table=table, k_out=k_out, v_out=v_out, **others) as s:
+        new = lambda: torch.empty((rows, Hkv, HEAD_DIM), dtype=torch.bfloat16, device=cache.k_codes.device)  # noqa: E731
+        k_out, v_out = new() if k_out is None else k_out, new() if v_out is None else v_out
+        rc = lib().w4a8_cache4_read(c, b, *_token_rows(k_out, "k_out"), *_token_rows(v_out, "v_out"), s.cuda_stream)
+    _check(rc, "w4a8_cache4_read")
+    return k_out, v_out
+
+
+def w4a8_cache4_attention_workspace_bytes(B: int, T: int, H: int, Hkv: int, max_len: int) -> int:
+    return int(lib().w4a8_cache4_attention_workspace_bytes(B, T, H, Hkv, max_len))
+
+
+def w4a8_cache4_attention(q: torch.Tensor, cache: KVCache4, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
+                          scale: float, max_len: int | None = None, out: torch.Tensor | None = None,
+                          workspace: Workspace | torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of a step's new tokens over the 4-bit cache that holds them
+    already (w4a8_cache4_append): q bf16 [T][H][128] (rotated already), strided
+    views allowed -> bf16 [T][H][128] (`out` may be a strided view too; rows of
+    no sequence are not written).  New token i of n of a sequence of length L
+    sees its tokens up to L - n + i.  max_len, an upper bound of the lengths (the
+    table's by default), only decides how the work is split."""
+    if stream is None:
+        buf, home, own = _workspace_of(workspace)
+        r = (_fast or _load_fast()).cache4_attention(q, cache, starts, lengths, table, scale, max_len, out, buf, home, own)
+        if type(r) is int and r < 0:  # the bytes that the Workspace, on this stream or still empty, lacks
+            with _unless_refused(workspace):
+                workspace.get(-r)
+                return w4a8_cache4_attention(q, cache, starts, lengths, table, scale, max_len, out, workspace)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "w4a8_cache4_attention")
+    q_rows = _token_rows(q, "q")
+    T, H = q.shape[0], q.shape[1]
+    c, Hkv = _cache4_args(cache)
+    b = _batch4_args(T, starts, lengths, table)
+    if max_len is None:
+        max_len = b.max_blocks * CACHE_BLOCK
+    if out is not None and out.shape != q.shape:
+        raise ValueError(f"out must be [{T}][{H}][{HEAD_DIM}]")
+    with _unless_refused(workspace), _call_on(stream, q, starts=starts, lengths=lengths, table=table, out=out, **cache._asdict()) as s:
+        if out is None:
+            out = torch.empty((T, H, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
+        need = w4a8_cache4_attention_workspace_bytes(b.B, T, H, Hkv, max_len)
+        _check_workspace_device(workspace, q.device)
+        wk_ptr, wk_bytes = _workspace_ptr(workspace, need, q.device, s)
+        rc = lib().w4a8_cache4_attention(c, b, *q_rows, H, float(scale), max_len, *_token_rows(out, "out"), wk_ptr, wk_bytes,
+                                         s.cuda_stream)
+        _check(rc, "w4a8_cache4_attention")
     return out

@@ -17,9 +17,10 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libw4a8.so")
 SOURCES = ["quantize.hip", "pack.hip", "gemm_smallm.hip", "gemm_largem.hip", "gemm_largem_group.hip",
-           "attention.hip", "cache.hip", "flow.hip", "noalloc.hip", "api.cpp"]
-# per-source extra flags: the group-scale GEMM and the cache attention use VGPR-form MFMAs
-EXTRA_FLAGS = {"gemm_largem_group.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "cache.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+           "attention.hip", "cache.hip", "cache4.hip", "heads.hip", "flow.hip", "noalloc.hip", "api.cpp"]
+# per-source extra flags: the group-scale GEMM and the caches' attention use VGPR-form MFMAs
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+EXTRA_FLAGS = {"gemm_largem_group.hip": VGPR_FORM, "cache.hip": VGPR_FORM, "cache4.hip": VGPR_FORM}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -10,6 +10,7 @@
 
 #include "attention.h"
 #include "cache.h"
+#include "cache4.h"
 #include "kernels.h"
 
 using namespace w4a8;
@@ -244,6 +245,70 @@ bool valid_rows(const uint16_t* p, int64_t row, int64_t head) {
   return p && aligned(p, 16) && row >= 0 && head >= 0 && row <= kMax && head <= kMax && row % 8 == 0 && head % 8 == 0;
 }
 
+// Token rows [T][heads][128] of given strides, in elements.
+struct Rows {
+  const uint16_t* p;
+  int64_t row, head, T, heads;
+  int64_t extent() const { return (T - 1) * row + (heads - 1) * head + kCacheD; }
+};
+Rows rows_of(const uint16_t* p, int64_t row, int64_t head, int64_t T, int64_t heads) {  // the stride of an axis of one is free
+  return {p, T == 1 ? kCacheD : row, heads == 1 ? kCacheD : head, T, heads};
+}
+// Rows apart from each other: heads within tokens, or tokens within heads.
+bool rows_apart(const Rows& a) {
+  constexpr int64_t D = kCacheD;
+  return ((a.heads == 1 || a.head >= D) && (a.T == 1 || a.row >= (a.heads - 1) * a.head + D)) ||
+         ((a.T == 1 || a.row >= D) && (a.heads == 1 || a.head >= (a.T - 1) * a.row + D));
+}
+// Two sets of rows that share no element, as far as that can be seen: disjoint
+// ranges, or equal strides with one set's places in the other's gaps.
+bool rows_disjoint(const Rows& a, const Rows& b) {
+  if (!overlap(a.p, (size_t)a.extent() * 2, b.p, (size_t)b.extent() * 2)) return true;
+  auto in_gaps = [&](int64_t stride, int64_t a_span, int64_t b_span) {
+    const int64_t bytes = 2 * stride, by = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+    const int64_t at = ((by % bytes) + bytes) % bytes / 2;  // (a multiple of 16 bytes apart)
+    return at >= a_span && at + b_span <= stride;
+  };
+  if (a.T > 1 && b.T > 1 && a.row == b.row && a.row > 0 &&
+      in_gaps(a.row, (a.heads - 1) * a.head + kCacheD, (b.heads - 1) * b.head + kCacheD))
+    return true;
+  return a.heads > 1 && b.heads > 1 && a.head == b.head && a.head > 0 &&
+         in_gaps(a.head, (a.T - 1) * a.row + kCacheD, (b.T - 1) * b.row + kCacheD);
+}
+
+// Sizes and pointers that the 4-bit cache's calls have in common.
+w4a8_status check_cache4(const w4a8_cache4* c, const w4a8_batch* b, Cache4Batch* out) {
+  if (!c || !b) return W4A8_EINVAL;
+  if (c->Hkv < 1 || c->Hkv > kCacheHeadsMax || c->n_pages < 1 || c->n_pages > kI32Max) return W4A8_EINVAL;
+  if (b->B < 0 || b->B > kCacheBatchMax || b->T < 0 || b->T > W4A8_M_MAX) return W4A8_EINVAL;
+  if (b->max_blocks < 1 || b->max_blocks > (int64_t(1) << 24)) return W4A8_EINVAL;
+  if (b->B == 0 || b->T == 0) return W4A8_OK;
+  if (!c->k_codes || !c->v_codes || !c->k_params || !c->v_params || !aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) ||
+      !aligned(c->k_params, 16) || !aligned(c->v_params, 16))
+    return W4A8_EINVAL;
+  if (!b->starts || !b->lengths || !b->table || !aligned(b->starts, 4) || !aligned(b->lengths, 4) || !aligned(b->table, 4))
+    return W4A8_EINVAL;
+  out->k_codes = c->k_codes;
+  out->v_codes = c->v_codes;
+  out->k_params = c->k_params;
+  out->v_params = c->v_params;
+  out->n_pages = c->n_pages;
+  out->starts = b->starts;
+  out->lengths = b->lengths;
+  out->table = b->table;
+  out->max_blocks = (int)b->max_blocks;
+  out->B = (int)b->B;
+  out->T = (int)b->T;
+  out->Hkv = (int)c->Hkv;
+  return W4A8_OK;
+}
+// Whether rows share no byte with the cache's arrays.
+bool apart_from_cache(const Rows& r, const w4a8_cache4* c) {
+  const size_t n = (size_t)r.extent() * 2, codes = (size_t)c->n_pages * c->Hkv * 4096, params = codes / 8;
+  return !overlap(r.p, n, c->k_codes, codes) && !overlap(r.p, n, c->v_codes, codes) && !overlap(r.p, n, c->k_params, params) &&
+         !overlap(r.p, n, c->v_params, params);
+}
+
 bool valid_cache_attention(int64_t B, int64_t T, int64_t H, int64_t Hkv, int64_t max_len) {
   return B >= 0 && B <= kCacheBatchMax && T >= 0 && T <= W4A8_M_MAX && Hkv >= 1 && H >= 1 && H <= kCacheHeadsMax &&
          H % Hkv == 0 && max_len >= 1 && max_len <= (int64_t(1) << 30);
@@ -462,6 +527,118 @@ w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batc
   a.max_len = (int)max_len;
   hipError_t error;
   if (!launch_cache_attention(a, workspace, workspace_bytes, stream, error)) return W4A8_EINVAL;
+  return error == hipSuccess ? W4A8_OK : W4A8_EHIP;
+}
+
+w4a8_status w4a8_qk_norm_rope(const w4a8_heads* q, const w4a8_heads* k, int64_t T, float eps, const w4a8_rope* rope,
+                              hipStream_t stream) {
+  if (T < 0 || T > W4A8_M_MAX) return W4A8_EINVAL;
+  if (!(eps > 0.0f) || !(eps <= 3.4e38f)) return W4A8_EINVAL;  // also rejects NaN and inf
+  const w4a8_heads* kinds[2] = {q && q->heads ? q : nullptr, k && k->heads ? k : nullptr};
+  for (const w4a8_heads* h : kinds)
+    if (h && (h->heads < 0 || h->heads > kCacheHeadsMax || (!h->gamma && !rope))) return W4A8_EINVAL;
+  QkNormRopeArgs a{};
+  if (rope) {
+    if (rope->n_axes < 1 || rope->n_axes > 4 || rope->n_pos < 1 || rope->n_pos > (int64_t(1) << 30)) return W4A8_EINVAL;
+    a.whole = true;
+    for (int i = 0; rope->axis && i < kCacheD / 2; ++i) {
+      const uint64_t x = rope->axis[i];
+      if ((int64_t)x >= rope->n_axes) return W4A8_EINVAL;
+      a.axis_lo |= (x & 1) << i;
+      a.axis_hi |= (x >> 1) << i;
+      a.whole = a.whole && x == rope->axis[i & ~7];
+    }
+  }
+  if (T == 0 || (!kinds[0] && !kinds[1])) return W4A8_OK;
+  if (rope) {
+    if (!rope->pos || !rope->rope_cos || !rope->rope_sin || !aligned(rope->pos, 4) || !aligned(rope->rope_cos, 16) ||
+        !aligned(rope->rope_sin, 16))
+      return W4A8_EINVAL;
+    a.pos = rope->pos;
+    a.rope_cos = rope->rope_cos;
+    a.rope_sin = rope->rope_sin;
+    a.n_pos = (int)rope->n_pos;
+    a.axes = (int)rope->n_axes;
+  }
+  Rows in[2], out[2];
+  HeadRows* to[2] = {&a.q, &a.k};
+  for (int i = 0; i < 2; ++i) {
+    const w4a8_heads* h = kinds[i];
+    if (!h) continue;
+    if (!valid_rows(h->x, h->row, h->head) || !valid_rows(h->out, h->out_row, h->out_head) || !aligned(h->gamma, 16))
+      return W4A8_EINVAL;
+    in[i] = rows_of(h->x, h->row, h->head, T, h->heads);
+    out[i] = rows_of(h->out, h->out_row, h->out_head, T, h->heads);
+    if (!rows_apart(out[i])) return W4A8_EINVAL;
+    *to[i] = {{const_cast<uint16_t*>(h->x), h->row, h->head}, {h->out, h->out_row, h->out_head}, h->gamma, (int)h->heads};
+  }
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+      if (!kinds[i] || !kinds[j]) continue;
+      const bool in_place = i == j && out[i].p == in[i].p && out[i].row == in[i].row && out[i].head == in[i].head;
+      if (!in_place && !rows_disjoint(out[i], in[j])) return W4A8_EINVAL;
+      if (i < j && !rows_disjoint(out[i], out[j])) return W4A8_EINVAL;
+    }
+  a.T = (int)T;
+  a.eps = eps;
+  return launch_qk_norm_rope(a, stream) == hipSuccess ? W4A8_OK : W4A8_EHIP;
+}
+
+w4a8_status w4a8_cache4_append(const w4a8_cache4* cache, const w4a8_batch* batch, const uint16_t* k, int64_t k_row,
+                               int64_t k_head, const uint16_t* v, int64_t v_row, int64_t v_head, hipStream_t stream) {
+  Cache4RowsArgs a{};
+  const w4a8_status s = check_cache4(cache, batch, &a.c);
+  if (s != W4A8_OK) return s;
+  if (batch->B == 0 || batch->T == 0) return W4A8_OK;
+  if (!valid_rows(k, k_row, k_head) || !valid_rows(v, v_row, v_head)) return W4A8_EINVAL;
+  a.k = {const_cast<uint16_t*>(k), k_row, k_head};
+  a.v = {const_cast<uint16_t*>(v), v_row, v_head};
+  return launch_cache4_append(a, stream) == hipSuccess ? W4A8_OK : W4A8_EHIP;
+}
+
+w4a8_status w4a8_cache4_read(const w4a8_cache4* cache, const w4a8_batch* batch, uint16_t* k, int64_t k_row, int64_t k_head,
+                             uint16_t* v, int64_t v_row, int64_t v_head, hipStream_t stream) {
+  Cache4RowsArgs a{};
+  const w4a8_status s = check_cache4(cache, batch, &a.c);
+  if (s != W4A8_OK) return s;
+  if (batch->B == 0 || batch->T == 0 || (!k && !v)) return W4A8_OK;
+  const Rows kr = rows_of(k, k_row, k_head, batch->T, cache->Hkv), vr = rows_of(v, v_row, v_head, batch->T, cache->Hkv);
+  if (k && (!valid_rows(k, k_row, k_head) || !rows_apart(kr) || !apart_from_cache(kr, cache))) return W4A8_EINVAL;
+  if (v && (!valid_rows(v, v_row, v_head) || !rows_apart(vr) || !apart_from_cache(vr, cache))) return W4A8_EINVAL;
+  if (k && v && !rows_disjoint(kr, vr)) return W4A8_EINVAL;
+  a.k = {k, k_row, k_head};
+  a.v = {v, v_row, v_head};
+  return launch_cache4_read(a, stream) == hipSuccess ? W4A8_OK : W4A8_EHIP;
+}
+
+size_t w4a8_cache4_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hkv, int64_t max_len) {
+  if (!valid_cache_attention(B, T, H, Hkv, max_len) || B == 0 || T == 0) return 0;
+  return cache4_attention_workspace((int)B, (int)T, (int)H, (int)Hkv, (int)max_len);
+}
+
+w4a8_status w4a8_cache4_attention(const w4a8_cache4* cache, const w4a8_batch* batch, const uint16_t* q, int64_t q_row,
+                                  int64_t q_head, int64_t H, float scale, int64_t max_len, uint16_t* o, int64_t o_row,
+                                  int64_t o_head, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  Cache4AttnArgs a{};
+  const w4a8_status s = check_cache4(cache, batch, &a.c);
+  if (s != W4A8_OK) return s;
+  if (!valid_cache_attention(batch->B, batch->T, H, cache->Hkv, max_len) ||
+      max_len > batch->max_blocks * W4A8_CACHE_BLOCK)
+    return W4A8_EINVAL;
+  if (!(scale == scale) || scale > 3.4e38f || scale < -3.4e38f) return W4A8_EINVAL;  // finite
+  if (batch->B == 0 || batch->T == 0) return W4A8_OK;
+  if (!valid_rows(q, q_row, q_head) || !valid_rows(o, o_row, o_head)) return W4A8_EINVAL;
+  if (!rows_apart(rows_of(o, o_row, o_head, batch->T, H))) return W4A8_EINVAL;
+  if (!cache_attention_fits(a.c.T, (int)H, a.c.Hkv)) return W4A8_EUNSUPPORTED;
+  a.q = {const_cast<uint16_t*>(q), q_row, q_head};
+  a.o = {o, o_row, o_head};
+  a.H = (int)H;
+  // as in w4a8_stream_attention, the queries carry the scale's sign, or its zero
+  a.scale_log2e = (scale == 0.0f ? 1.0f : std::fabs(scale)) * 1.4426950408889634f;
+  a.q_sign = scale == 0.0f ? 0.0f : scale < 0.0f ? -1.0f : 1.0f;
+  a.max_len = (int)max_len;
+  hipError_t error;
+  if (!launch_cache4_attention(a, workspace, workspace_bytes, stream, error)) return W4A8_EINVAL;
   return error == hipSuccess ? W4A8_OK : W4A8_EHIP;
 }
 

@@ -311,6 +311,210 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// The 4-bit cache's: (k_codes, v_codes, k_params, v_params), and a batch's
+// (starts, lengths, table).
+bool cache4_view(PyObject* o, c10::DeviceIndex device, w4a8_cache4& c) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
+  auto item = [&](int i) { return PyTuple_GET_ITEM(o, i); };
+  const at::Tensor *k = whole(item(0), at::kInt, 5, device), *v = whole(item(1), at::kInt, 6, device),
+                   *kp = whole(item(2), at::kHalf, 5, device), *vp = whole(item(3), at::kHalf, 5, device);
+  if (!k || !v || !kp || !vp) return false;
+  const int64_t pages = k->size(0), Hkv = k->size(1);
+  auto is = [&](const at::Tensor* t, std::initializer_list<int64_t> shape) {
+    int64_t i = 2;
+    for (int64_t n : shape)
+      if (t->size(i++) != n) return false;
+    return t->size(0) == pages && t->size(1) == Hkv;
+  };
+  if (!is(k, {4, 16, 16}) || !is(v, {8, 2, 16, 4}) || !is(kp, {2, W4A8_CACHE_BLOCK, 2}) || !is(vp, {2, 2, W4A8_CACHE_BLOCK}))
+    return false;
+  c = {ptr<uint32_t>(k), ptr<uint32_t>(v), ptr<uint16_t>(kp), ptr<uint16_t>(vp), pages, Hkv};
+  return true;
+}
+bool batch4_view(PyObject* const* b, int64_t T, c10::DeviceIndex device, w4a8_batch& out) {
+  const at::Tensor *starts = whole(b[0], at::kInt, 1, device), *lengths = whole(b[1], at::kInt, 1, device),
+                   *table = whole(b[2], at::kInt, 2, device);
+  if (!starts || !lengths || !table) return false;
+  const int64_t B = lengths->size(0);
+  if (starts->size(0) != B + 1 || table->size(0) != B) return false;
+  out = {ptr<int32_t>(starts), ptr<int32_t>(lengths), ptr<int32_t>(table), table->size(1), B, T, nullptr, nullptr, nullptr, 0};
+  return true;
+}
+const at::Tensor* token_rows(PyObject* o, c10::DeviceIndex device) {
+  const at::Tensor* t = rows_of(o, at::kBFloat16, 3, device);
+  return t && t->size(2) == 128 ? t : nullptr;
+}
+
+// cache4_append(k, v, cache, starts, lengths, table) -> True
+PyObject* cache4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const c10::DeviceIndex device = n == 6 ? device_of(a[0]) : -1;
+  if (device < 0) Py_RETURN_NONE;
+  const at::Tensor *k = token_rows(a[0], device), *v = token_rows(a[1], device);
+  w4a8_cache4 c;
+  w4a8_batch b;
+  if (!k || !v || k->sizes() != v->sizes() || !cache4_view(a[2], device, c) || k->size(1) != c.Hkv ||
+      !batch4_view(a + 3, k->size(0), device, b))
+    Py_RETURN_NONE;
+  const hipStream_t stream = current_stream();
+  const w4a8_status s = without_gil([&] {
+    return w4a8_cache4_append(&c, &b, ptr<uint16_t>(k), stride_of(k, 0), stride_of(k, 1), ptr<uint16_t>(v), stride_of(v, 0),
+                              stride_of(v, 1), stream);
+  });
+  if (s != W4A8_OK) return PyLong_FromLong(s);
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// Two results: the caller's own tensors, or the call's.
+PyObject* pair_of(PyObject* own0, const at::Tensor& t0, PyObject* own1, const at::Tensor& t1) {
+  PyObject* r = PyTuple_New(2);
+  if (!r) return nullptr;
+  PyTuple_SET_ITEM(r, 0, own0 != Py_None || !t0.defined() ? Py_NewRef(own0) : THPVariable_Wrap(t0));
+  PyTuple_SET_ITEM(r, 1, own1 != Py_None || !t1.defined() ? Py_NewRef(own1) : THPVariable_Wrap(t1));
+  return r;
+}
+
+// cache4_read(cache, starts, lengths, table, rows, k_out, v_out) -> (k, v)
+PyObject* cache4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7 || !is_int(a[4]) || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 4) Py_RETURN_NONE;
+  const c10::DeviceIndex device = device_of(PyTuple_GET_ITEM(a[0], 0));
+  const int64_t T = as_int(a[4]);
+  if (PyErr_Occurred()) PyErr_Clear();
+  if (device < 0 || T < 0) Py_RETURN_NONE;
+  w4a8_cache4 c;
+  w4a8_batch b;
+  if (!cache4_view(a[0], device, c) || !batch4_view(a + 1, T, device, b)) Py_RETURN_NONE;
+  const at::Tensor* own[2] = {nullptr, nullptr};
+  for (int i = 0; i < 2; ++i)
+    if (a[5 + i] != Py_None &&
+        (!(own[i] = token_rows(a[5 + i], device)) || own[i]->size(0) != T || own[i]->size(1) != c.Hkv))
+      Py_RETURN_NONE;
+  const at::Tensor& codes = THPVariable_Unpack(PyTuple_GET_ITEM(a[0], 0));
+  const hipStream_t stream = current_stream();
+  at::Tensor k, v;
+  const w4a8_status s = without_gil([&] {
+    k = own[0] ? *own[0] : at::empty({T, c.Hkv, 128}, codes.options().dtype(at::kBFloat16));
+    v = own[1] ? *own[1] : at::empty({T, c.Hkv, 128}, codes.options().dtype(at::kBFloat16));
+    return w4a8_cache4_read(&c, &b, ptr<uint16_t>(&k), stride_of(&k, 0), stride_of(&k, 1), ptr<uint16_t>(&v), stride_of(&v, 0),
+                            stride_of(&v, 1), stream);
+  });
+  if (s != W4A8_OK) return PyLong_FromLong(s);
+  return pair_of(a[5], k, a[6], v);
+  END_HANDLE_TH_ERRORS
+}
+
+// qk_norm_rope(q, k, gamma_q, gamma_k, eps, pos, rope_cos, rope_sin, axes, q_out, k_out) -> (q, k)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 11 || !PyFloat_CheckExact(a[4])) Py_RETURN_NONE;
+  const c10::DeviceIndex device = device_of(a[0] != Py_None ? a[0] : a[1]);
+  if (device < 0) Py_RETURN_NONE;
+  w4a8_heads heads[2] = {};
+  const at::Tensor *x[2] = {nullptr, nullptr}, *own[2] = {nullptr, nullptr};
+  int64_t T = -1;
+  for (int i = 0; i < 2; ++i) {
+    if (a[i] == Py_None) continue;
+    if (!(x[i] = token_rows(a[i], device)) || (T >= 0 && x[i]->size(0) != T)) Py_RETURN_NONE;
+    T = x[i]->size(0);
+    heads[i] = {ptr<uint16_t>(x[i]), stride_of(x[i], 0), stride_of(x[i], 1), x[i]->size(1), nullptr, nullptr, 0, 0};
+    if (a[2 + i] != Py_None) {
+      const at::Tensor* gamma = whole(a[2 + i], at::kBFloat16, 1, device);
+      if (!gamma || gamma->size(0) != 128) Py_RETURN_NONE;
+      heads[i].gamma = ptr<uint16_t>(gamma);
+    }
+    if (a[9 + i] != Py_None && (!(own[i] = token_rows(a[9 + i], device)) || own[i]->sizes() != x[i]->sizes())) Py_RETURN_NONE;
+  }
+  w4a8_rope rope = {};
+  if (a[5] != Py_None) {
+    const at::Tensor* pos = whole(a[5], at::kInt, 2, device);
+    if (!pos) pos = whole(a[5], at::kInt, 1, device);
+    const at::Tensor *cs = whole(a[6], at::kFloat, 2, device), *sn = whole(a[7], at::kFloat, 2, device);
+    if (!pos || !cs || !sn || pos->size(pos->dim() - 1) != T || cs->sizes() != sn->sizes() || cs->size(1) != 64) Py_RETURN_NONE;
+    if (a[8] != Py_None && (!PyBytes_CheckExact(a[8]) || PyBytes_GET_SIZE(a[8]) != 64)) Py_RETURN_NONE;
+    rope = {ptr<int32_t>(pos), pos->dim() == 2 ? pos->size(0) : 1,
+            a[8] == Py_None ? nullptr : reinterpret_cast<const uint8_t*>(PyBytes_AS_STRING(a[8])), ptr<float>(cs), ptr<float>(sn),
+            cs->size(0)};
+  }
+  const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
+  const hipStream_t stream = current_stream();
+  at::Tensor y[2];
+  const w4a8_status s = without_gil([&] {
+    for (int i = 0; i < 2; ++i)
+      if (x[i]) {
+        y[i] = own[i] ? *own[i] : at::empty(x[i]->sizes(), x[i]->options());
+        heads[i].out = ptr<uint16_t>(&y[i]);
+        heads[i].out_row = stride_of(&y[i], 0);
+        heads[i].out_head = stride_of(&y[i], 1);
+      }
+    return w4a8_qk_norm_rope(x[0] ? &heads[0] : nullptr, x[1] ? &heads[1] : nullptr, T, eps, a[5] == Py_None ? nullptr : &rope, stream);
+  });
+  if (s != W4A8_OK) return PyLong_FromLong(s);
+  return pair_of(x[0] ? a[9] : Py_None, y[0], x[1] ? a[10] : Py_None, y[1]);
+  END_HANDLE_TH_ERRORS
+}
+
+// cache4_attention(q, cache, starts, lengths, table, scale, max_len, out,
+//                  workspace, workspace_stream, is_workspace)
+// The last three and a negative answer are as for linear.
+PyObject* cache4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const c10::DeviceIndex device = n == 11 ? device_of(a[0]) : -1;
+  if (device < 0) Py_RETURN_NONE;
+  const at::Tensor *q = token_rows(a[0], device), *out = nullptr;
+  w4a8_cache4 c;
+  w4a8_batch b;
+  if (!q || !cache4_view(a[1], device, c) || !batch4_view(a + 2, q->size(0), device, b) || !PyFloat_CheckExact(a[5])) Py_RETURN_NONE;
+  const int64_t T = b.T, H = q->size(1);
+  int64_t max_len = b.max_blocks * W4A8_CACHE_BLOCK;
+  if (a[6] != Py_None) {
+    if (!is_int(a[6])) Py_RETURN_NONE;
+    max_len = as_int(a[6]);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+  }
+  if (a[7] != Py_None && (!(out = token_rows(a[7], device)) || out->sizes() != q->sizes())) Py_RETURN_NONE;
+  const float scale = (float)PyFloat_AS_DOUBLE(a[5]);
+  const hipStream_t stream = current_stream();
+  const size_t need = w4a8_cache4_attention_workspace_bytes(b.B, T, H, c.Hkv, max_len);
+  void* wk = nullptr;
+  size_t wk_bytes = 0;
+  const bool temporary = need && a[8] == Py_None && a[10] != Py_True;
+  if (need && !temporary) {
+    const at::Tensor* buf = plain(a[8], at::kByte);
+    if (!buf || buf->get_device() != device) Py_RETURN_NONE;
+    if (a[10] == Py_True) {
+      if (a[9] != Py_None && (!is_int(a[9]) || PyLong_AsVoidPtr(a[9]) != (void*)stream)) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+      }
+      if ((size_t)buf->numel() < need) return PyLong_FromLongLong(-(long long)need);
+      if (a[9] == Py_None) Py_RETURN_NONE;
+    }
+    wk = buf->data_ptr();
+    wk_bytes = (size_t)buf->numel();
+  }
+  at::Tensor y;
+  const w4a8_status s = without_gil([&] {
+    y = out ? *out : at::empty({T, H, 128}, q->options());
+    at::Tensor tmp;  // released to the allocator on this stream, which orders its next use
+    if (temporary) {
+      tmp = at::empty({(int64_t)need}, q->options().dtype(at::kByte));
+      wk = tmp.data_ptr();
+      wk_bytes = need;
+    }
+    return w4a8_cache4_attention(&c, &b, ptr<uint16_t>(q), stride_of(q, 0), stride_of(q, 1), H, scale, max_len, ptr<uint16_t>(&y),
+                                 stride_of(&y, 0), stride_of(&y, 1), wk, wk_bytes, stream);
+  });
+  if (s != W4A8_OK) return PyLong_FromLong(s);
+  if (out) return Py_NewRef(a[7]);
+  return THPVariable_Wrap(std::move(y));
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* pair(at::Tensor q, at::Tensor s) {
   PyObject* t = PyTuple_New(2);
   if (!t) return nullptr;
@@ -390,6 +594,10 @@ PyMethodDef methods[] = {{"linear", FAST(linear), nullptr},
                          {"add_norm", FAST(add_norm), nullptr},
                          {"cache_append", FAST(cache_append), nullptr},
                          {"cache_attention", FAST(cache_attention), nullptr},
+                         {"qk_norm_rope", FAST(qk_norm_rope), nullptr},
+                         {"cache4_append", FAST(cache4_append), nullptr},
+                         {"cache4_read", FAST(cache4_read), nullptr},
+                         {"cache4_attention", FAST(cache4_attention), nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

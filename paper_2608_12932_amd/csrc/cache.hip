@@ -13,8 +13,7 @@
 #include <algorithm>
 #include <climits>
 
-#include "cache.h"
-#include "device.h"
+#include "cache_device.h"
 #include "kernels.h"
 
 namespace w4a8 {
@@ -23,72 +22,6 @@ namespace {
 
 constexpr int kD = kCacheD, kHalf = kD / 2, kBlock = kCacheBlock, kRecent = kCacheRecent;
 constexpr int kPageBytes = kBlock * kD;  // one head's codes of a page, keys or values
-
-// ---- the batch
-
-struct Sequence {
-  int b;     // -1: none
-  int row0;  // first row of its new tokens
-  int n;     // new tokens
-  int len;   // tokens held, the new ones the last of them
-  int item;  // the item's number within the sequence
-};
-
-// Rows and length of sequence b; whatever the arrays hold, the rows lie in
-// [0, T) and the length within the table.
-__device__ __forceinline__ void sequence(const CacheBatch& c, int b, int& row0, int& n, int& len) {
-  row0 = min(max(c.starts[b], 0), c.T);
-  n = min(max(c.starts[b + 1], row0), c.T) - row0;
-  len = min(max(c.lengths[b], 0), c.max_blocks * kBlock);
-}
-
-// Inclusive sum over the wave's lanes, by lane moves in the vector unit: within
-// rows of 16, then each row's total into the rows after it.
-__device__ __forceinline__ int wave_scan(int v) {
-  constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
-  auto step = [&](auto ctrl, auto rows) {  // lanes without a source add 0
-    v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
-  };
-  using std::integral_constant;
-  step(integral_constant<int, kRowShr + 1>{}, integral_constant<int, 0xF>{});
-  step(integral_constant<int, kRowShr + 2>{}, integral_constant<int, 0xF>{});
-  step(integral_constant<int, kRowShr + 4>{}, integral_constant<int, 0xF>{});
-  step(integral_constant<int, kRowShr + 8>{}, integral_constant<int, 0xF>{});
-  step(integral_constant<int, kRowBcast15>{}, integral_constant<int, 0xA>{});
-  step(integral_constant<int, kRowBcast31>{}, integral_constant<int, 0xC>{});
-  return v;
-}
-
-// The sequence that work item `item` belongs to, when sequence b has
-// count(n, len) items and they are numbered through the batch.  Every wave
-// finds it by itself, 64 sequences at a time.
-template <class F>
-__device__ __forceinline__ Sequence find_sequence(const CacheBatch& c, int item, F count) {
-  const int lane = threadIdx.x & 63;
-  int base = 0;
-  for (int b0 = 0; b0 < c.B; b0 += 64) {
-    const int b = b0 + lane;
-    int row0 = 0, n = 0, len = 0, cnt = 0;
-    if (b < c.B) {
-      sequence(c, b, row0, n, len);
-      cnt = count(n, len);
-    }
-    const int upto = wave_scan(cnt);
-    const uint64_t past = __ballot(base + upto > item);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      Sequence s;
-      s.b = b0 + l;
-      s.row0 = __builtin_amdgcn_readlane(row0, l);
-      s.n = __builtin_amdgcn_readlane(n, l);
-      s.len = __builtin_amdgcn_readlane(len, l);
-      s.item = item - base - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(cnt, l));
-      return s;
-    }
-    base += __builtin_amdgcn_readlane(upto, 63);
-  }
-  return Sequence{-1, 0, 0, 0, 0};
-}
 
 __device__ __forceinline__ int clamp_pos(int p, int n_pos) { return p < 0 ? 0 : (p >= n_pos ? n_pos - 1 : p); }
 
@@ -254,10 +187,6 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append(const CacheAppend
 
 // ---- attention
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 // Weights are exp2(score - offset) 2^12.  The offset follows the running maximum
 // only where that has outgrown it by more than 3, so that the sums are hardly
 // ever rescaled: weights reach 2^15 at most, and fp16 holds those down to
@@ -269,7 +198,7 @@ constexpr float kWeightShift = 12.0f, kSlack = 3.0f;
 // offset, and two scales are 2^80 apart at most.  Past that range a block whose
 // largest weight lies more than kFar below the offset adds to the total apart
 // from its weights, in rows that have seen such a scale.
-constexpr float kLowScale = 0x1p-60f, kHighScale = 0x1p20f, kLowLog2 = -60.0f, kHighLog2 = 20.0f, kFar = 100.0f;
+constexpr float kLowScale = 0x1p-60f, kHighScale = 0x1p20f, kLowLog2 = -60.0f, kHighLog2 = 20.0f;
 // stand-in scale of a values' block of zeros: its weights still count
 constexpr float kZeroLog2 = kLowLog2, kZeroInv = 1.0f / kLowScale;
 // Exponents are score factor + (log2 of the values' scale + 12 - offset), one
@@ -280,7 +209,8 @@ constexpr float kLarge = 0x1p16f;
 // The total is held times 2^-15: a token whose weight is at the offset then adds
 // 2^-3 / scale, up to 2^97 with the smallest scale there is and the slack, so
 // that 2^30 of them stay below 2^128, and 2^-103 with a scale of 2^100.
-constexpr float kTotalUnit = 0x1p-15f, kTotalShift = kWeightShift - 15.0f;
+// (kTotalUnit.)
+constexpr float kTotalShift = kWeightShift - 15.0f;
 
 __device__ __forceinline__ f16x2 as_f16x2(uint32_t u) { return __builtin_bit_cast(f16x2, u); }
 
@@ -298,36 +228,6 @@ __device__ __forceinline__ f16x8 codes_to_f16x8(uint32_t w0, uint32_t w1) {
   codes_to_f16(w1, r.z, r.w);
   return __builtin_bit_cast(f16x8, r);
 }
-// Two weights to fp16, round to nearest even.
-__device__ __forceinline__ uint32_t f16x2_bits(float lo, float hi) {
-  const float2_t v = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
-}
-
-// Eight elements of a row's output from its sums and total.  A row that sees
-// nothing is 0 (0 * 0), NaN stays.
-__device__ __forceinline__ uint4 output8(const float (&o)[8], float total) {
-  const float inv = total > 0.0f ? 1.0f / total : total;
-  auto two = [&](int e) { return bf16x2_bits(o[e] * kTotalUnit * inv, o[e + 1] * kTotalUnit * inv); };
-  return make_uint4(two(0), two(2), two(4), two(6));
-}
-
-// A total moved by the factor 2^d, d <= 0: by one product, or, where that would
-// vanish while the total (which may be as large as 2^127) does not, by two.
-__device__ __forceinline__ float rescaled(float total, float d) {
-  const float half = __builtin_amdgcn_exp2f(0.5f * d);
-  return d < -kFar ? total * half * half : total * __builtin_amdgcn_exp2f(d);
-}
-
-// The larger (sum) of the values of lanes l, l ^ 16, l ^ 32 and l ^ 48.
-template <class F>
-__device__ __forceinline__ float fold_groups(float x, F op) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return op(__uint_as_float(t[0]), __uint_as_float(t[1]));
-}
-
 // One workgroup per (rows of one sequence's kv head, split of its blocks).
 // A row is a (new token, query head of the kv head) pair, row i G + g; a wave
 // holds R tiles of 16 rows.  Of NW waves KW hold the same rows and take every
@@ -844,80 +744,6 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attention(const CacheAttnArg
   }
 }
 
-// Merge of the splits' partial results, [S][T][H]: P threads for 8 d of a
-// (token, head), each folding every P-th split, their results meeting by lane
-// moves and, from four waves, in LDS.  (One thread for all of 64 splits took
-// 36 us of the 79 that one token over 100000 took: its reads wait for each
-// other.)  Tokens of no sequence are left as they are.
-template <int P>
-__global__ __launch_bounds__(256) void cache_attention_merge(const CacheAttnArgs a) {
-  constexpr int kChunks = kD / 8, kRowsHere = 256 / (kChunks * P);
-  static_assert(P == 4 || P == 16, "parts of a row are the four 16-lane groups of one or four waves");
-  struct Partial {
-    float mx, sum, o[8];
-  };
-  constexpr int kWords = sizeof(Partial) / 4;
-  struct Words {
-    uint32_t w[kWords];
-  };
-  __shared__ uint32_t l_part[P == 16 ? 4 : 1][kWords][kChunks];
-  const int tid = threadIdx.x, c = tid % kChunks, part = tid / kChunks % P;
-  const int64_t row = (int64_t)blockIdx.x * kRowsHere + tid / (kChunks * P), rows = (int64_t)a.c.T * a.H;
-  const int64_t tok = row / a.H;
-  const int first = a.c.starts[0], end = a.c.starts[a.c.B];
-  auto fold = [](const Partial& x, const Partial& y) {
-    Partial r;
-    r.mx = fmaxf(x.mx, y.mx);
-    const float base = r.mx == -INFINITY ? 0.0f : r.mx;
-    const float f0 = __builtin_amdgcn_exp2f(x.mx - base), f1 = __builtin_amdgcn_exp2f(y.mx - base);
-    r.sum = rescaled(x.sum, x.mx - base) + rescaled(y.sum, y.mx - base);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.o[e] = x.o[e] * f0 + y.o[e] * f1;
-    return r;
-  };
-  Partial mine{-INFINITY, 0.0f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-  if (row < rows)
-    for (int s = part; s < a.S; s += P) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (s * rows + row) * 2);
-      const float4* p = reinterpret_cast<const float4*>(a.part_o + (s * rows + row) * kD + 8 * c);
-      const float4 u = p[0], v = p[1];
-      mine = fold(mine, Partial{ml.x, ml.y, {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w}});
-    }
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {  // lane groups 16, then 32 apart: a swap yields both values
-    const Words w = __builtin_bit_cast(Words, mine);
-    Words x, y;
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      const auto r = half == 0 ? __builtin_amdgcn_permlane16_swap(w.w[i], w.w[i], false, false)
-                               : __builtin_amdgcn_permlane32_swap(w.w[i], w.w[i], false, false);
-      x.w[i] = r[0];
-      y.w[i] = r[1];
-    }
-    mine = fold(__builtin_bit_cast(Partial, x), __builtin_bit_cast(Partial, y));
-  }
-  if constexpr (P == 16) {
-    if ((tid & 63) < kChunks) {
-      const Words w = __builtin_bit_cast(Words, mine);
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) l_part[tid >> 6][i][c] = w.w[i];
-    }
-    lds_barrier();
-    if (tid >= kChunks) return;
-#pragma unroll
-    for (int q = 1; q < 4; ++q) {
-      Words w;
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) w.w[i] = l_part[q][i][c];
-      mine = fold(mine, __builtin_bit_cast(Partial, w));
-    }
-  } else if (part != 0) {
-    return;
-  }
-  if (row >= rows || tok < first || tok >= end) return;
-  *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + (row % a.H) * a.o.head + 8 * c) = output8(mine.o, mine.sum);
-}
-
 // The forms of a call, and what one of its workgroups costs in ns: alone on a
 // CU lat + lat_round a round (a block of each of the KW groups of waves); in
 // a full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
@@ -1037,7 +863,7 @@ bool launch_cache_attention(const CacheAttnArgs& a0, void* workspace, size_t byt
   if (a.S > 1) {
     const int P = a.S <= 16 ? 4 : 16;
     const int64_t threads = (int64_t)a.c.T * a.H * (kD / 8) * P;
-    const AttnFn merge = P == 4 ? cache_attention_merge<4> : cache_attention_merge<16>;
+    const AttnFn merge = P == 4 ? cache_attention_merge<4, CacheAttnArgs> : cache_attention_merge<16, CacheAttnArgs>;
     merge<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream>>>(a);
   }
   error = hipGetLastError();

@@ -1,0 +1,700 @@
+// The 4-bit key/value cache: appending to it, reading it back and attending
+// over it.
+//
+// A sequence's cache is a list of blocks of 64 tokens, each a page of a pool
+// (the table names them).  Each token's keys and values of a kv head are held
+// by themselves, in two groups of 64 elements with an fp16 scale s and offset b:
+//     s = fp16((hi - lo) / 15),  b = fp16(lo - 16 s),
+//     code = min(max(round_half_even((x - b) / s - 16), 0), 15)  (0 where s = 0),
+// and stand for fp16(s (16 + code) + b).  A token's codes depend on nothing but
+// the token, so an append writes its tokens' codes and leaves all others.
+//
+// The sum 16 + code is what four bits in the mantissa of 16.0 in fp16 are, so a
+// value takes one masked insertion and one multiply-add in fp16, two at a time.
+#include <algorithm>
+#include <climits>
+
+#include "cache4.h"
+#include "cache_device.h"
+#include "kernels.h"
+
+namespace w4a8 {
+
+namespace {
+
+constexpr int kD = kCacheD, kBlock = kCacheBlock;
+constexpr int kCodeBytes = kBlock * kD / 2, kCodeWords = kCodeBytes / 4;  // one head's codes of a page, keys or values
+constexpr int kParams = 4 * kBlock, kParamBytes = 2 * kParams;            // and its scales and offsets
+constexpr float kClamp = 16384.0f;  // 16 s and b stay within fp16 up to here
+
+__device__ __forceinline__ f16x2 as_f16x2(uint32_t u) { return __builtin_bit_cast(f16x2, u); }
+
+// Eight values from a word: element 2 i in bits 4 i .., element 2 i + 1 in bits
+// 16 + 4 i ..; s[i] and b[i] are the scales and offsets of elements 2 i, 2 i + 1.
+__device__ __forceinline__ f16x8 values8(uint32_t w, const f16x2 (&s)[4], const f16x2 (&b)[4]) {
+  constexpr uint32_t kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;
+  const uint32_t f[4] = {((w << 6) & kMask) | kSixteen, ((w << 2) & kMask) | kSixteen, ((w >> 2) & kMask) | kSixteen,
+                         ((w >> 6) & kMask) | kSixteen};
+  uint4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_f16x2(f[0]), s[0], b[0]));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_f16x2(f[1]), s[1], b[1]));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_f16x2(f[2]), s[2], b[2]));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_f16x2(f[3]), s[3], b[3]));
+  return __builtin_bit_cast(f16x8, r);
+}
+// Eight keys: a word of one token, whose scale and offset are the halves of sb.
+__device__ __forceinline__ f16x8 keys8(uint32_t w, uint32_t sb) {
+  const f16x2 p = as_f16x2(sb), s2 = {p[0], p[0]}, b2 = {p[1], p[1]};
+  const f16x2 s[4] = {s2, s2, s2, s2}, b[4] = {b2, b2, b2, b2};
+  return values8(w, s, b);
+}
+// A value of eight tokens.
+__device__ __forceinline__ f16x8 values8(uint32_t w, const uint4& s4, const uint4& b4) {
+  const f16x2 s[4] = {as_f16x2(s4.x), as_f16x2(s4.y), as_f16x2(s4.z), as_f16x2(s4.w)};
+  const f16x2 b[4] = {as_f16x2(b4.x), as_f16x2(b4.y), as_f16x2(b4.z), as_f16x2(b4.w)};
+  return values8(w, s, b);
+}
+__device__ __forceinline__ int nibble(int e) { return 4 * (e >> 1) + 16 * (e & 1); }  // bits of element e
+
+// Items of append and read: the aligned groups of eight tokens that a
+// sequence's last n tokens touch.
+constexpr int kEight = 8;
+__device__ __forceinline__ int eights(int n, int len) {
+  return n > 0 && len > 0 ? (len - 1) / kEight - max(len - n, 0) / kEight + 1 : 0;
+}
+
+// ---- append
+
+// One workgroup per (eight tokens, kv head): half of its threads take the keys,
+// half the values, 16 threads to a token.
+__global__ __launch_bounds__(256) void cache4_append(const Cache4RowsArgs a) {
+  constexpr int kPitch = kD + 4;  // bytes of a token's codes in LDS, off the banks' period
+  __shared__ uint8_t l_codes[kEight * kPitch];
+  const Cache4Batch& cb = a.c;
+  const int tid = threadIdx.x & 127, hk = blockIdx.y;
+  const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7) == 0;
+  const Sequence s = find_sequence(cb, blockIdx.x, [](int n, int len) { return eights(n, len); });
+  if (s.b < 0) return;
+  const int first = max(s.len - s.n, 0);  // the first new token that has a place
+  const int t8 = first / kEight + s.item, page = cb.table[(int64_t)s.b * cb.max_blocks + t8 / (kBlock / kEight)];
+  const int c = tid & 15, t = t8 * kEight + (tid >> 4);
+  const bool there = t >= first && t < s.len;
+
+  // ---- the token's eight elements; one outside the call takes its last
+  const TokenRows rows = keys ? a.k : a.v;
+  const int64_t row = s.row0 + (there ? t - (s.len - s.n) : s.n - 1);
+  const uint4 x4 = *reinterpret_cast<const uint4*>(rows.p + row * rows.row + hk * rows.head + 8 * c);
+  const uint32_t xw[4] = {x4.x, x4.y, x4.z, x4.w};
+  float x[8], lo, hi;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float v = (e & 1) ? bf16_hi(xw[e / 2]) : bf16_lo(xw[e / 2]);
+    x[e] = v != v ? 0.0f : fminf(fmaxf(v, -kClamp), kClamp);
+    lo = e ? fminf(lo, x[e]) : x[e];
+    hi = e ? fmaxf(hi, x[e]) : x[e];
+  }
+  auto fold = [&](auto ctrl) {  // over the group's 8 lanes
+    lo = fminf(lo, __uint_as_float(lane_move<decltype(ctrl)::value>(__float_as_uint(lo))));
+    hi = fmaxf(hi, __uint_as_float(lane_move<decltype(ctrl)::value>(__float_as_uint(hi))));
+  };
+  fold(std::integral_constant<int, kXor1>{});
+  fold(std::integral_constant<int, kXor2>{});
+  fold(std::integral_constant<int, kMirror8>{});
+  const _Float16 s16 = (_Float16)((hi - lo) / 15.0f);
+  const float sf = (float)s16;
+  const _Float16 b16 = (_Float16)(lo - 16.0f * sf);  // (16 s is exact, so a fused difference is the same)
+  const float bf = (float)b16;
+  uint32_t code[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma clang fp contract(off)
+    const float q = rintf((x[e] - bf) / (sf > 0.0f ? sf : 1.0f) - 16.0f);
+    code[e] = sf > 0.0f ? (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f) : 0u;
+  }
+
+  const bool held = page >= 0 && page < cb.n_pages;
+  const int64_t head = (int64_t)(held ? page : 0) * cb.Hkv + hk;
+  const int at = t & (kBlock - 1);
+  const uint32_t s_bits = __builtin_bit_cast(uint16_t, s16), b_bits = __builtin_bit_cast(uint16_t, b16);
+  // ---- values: a thread turns eight tokens' codes of one d into a word
+  uint32_t* word = cb.v_codes + head * kCodeWords + (t8 & 7) * kD + tid;
+  uint32_t mask = 0, old = 0;  // the new tokens' bits, and what else the word holds
+  if (!keys) {
+    uint32_t* l = reinterpret_cast<uint32_t*>(l_codes + (tid >> 4) * kPitch) + 2 * c;
+    l[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+    l[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+#pragma unroll
+    for (int e = 0; e < kEight; ++e) mask |= t8 * kEight + e >= first && t8 * kEight + e < s.len ? 15u << nibble(e) : 0u;
+    if (held && mask != ~0u) old = *word & ~mask;
+  }
+  lds_barrier();
+  if (!held) return;
+  uint32_t w = 0;
+  if (keys) {
+    if (!there) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w |= code[e] << nibble(e);
+    cb.k_codes[head * kCodeWords + ((at & 3) * 16 + (at >> 2)) * 16 + c] = w;
+    if ((c & 7) == 0) reinterpret_cast<uint32_t*>(cb.k_params)[head * (kParams / 2) + (c >> 3) * kBlock + at] = s_bits | b_bits << 16;
+    return;
+  }
+  const int d = 8 * (tid >> 2 & 15) + 4 * (tid >> 6) + (tid & 3);
+#pragma unroll
+  for (int e = 0; e < kEight; ++e) w |= (uint32_t)l_codes[e * kPitch + d] << nibble(e);
+  *word = old | (w & mask);
+  if (there && (c & 7) == 0) {
+    uint16_t* p = cb.v_params + head * kParams + (c >> 3) * (2 * kBlock) + at;
+    p[0] = (uint16_t)s_bits;
+    p[kBlock] = (uint16_t)b_bits;
+  }
+}
+
+// ---- read
+
+// One workgroup per (eight tokens, kv head), 16 threads to a token's keys or
+// values.  The eight tokens of a word of values are eight threads' that read
+// it each, from the first cache.
+__global__ __launch_bounds__(256) void cache4_read(const Cache4RowsArgs a) {
+  const Cache4Batch& cb = a.c;
+  const int tid = threadIdx.x & 127, hk = blockIdx.y;
+  const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7) == 0;
+  const TokenRows rows = keys ? a.k : a.v;
+  if (!rows.p) return;
+  const Sequence s = find_sequence(cb, blockIdx.x, [](int n, int len) { return eights(n, len); });
+  if (s.b < 0) return;
+  const int first = max(s.len - s.n, 0), t8 = first / kEight + s.item;
+  const int page = cb.table[(int64_t)s.b * cb.max_blocks + t8 / (kBlock / kEight)];
+  const int c = tid & 15, t = t8 * kEight + (tid >> 4), at = t & (kBlock - 1);
+  if (t < first || t >= s.len) return;
+  uint4 out = make_uint4(0u, 0u, 0u, 0u);
+  if (page >= 0 && page < cb.n_pages) {
+    const int64_t head = (int64_t)page * cb.Hkv + hk;
+    f16x8 v;
+    if (keys) {
+      v = keys8(cb.k_codes[head * kCodeWords + ((at & 3) * 16 + (at >> 2)) * 16 + c],
+                reinterpret_cast<const uint32_t*>(cb.k_params)[head * (kParams / 2) + (c >> 3) * kBlock + at]);
+    } else {
+      const uint32_t* w = cb.v_codes + head * kCodeWords + (t8 & 7) * kD + 4 * c;
+      const uint4 w0 = *reinterpret_cast<const uint4*>(w), w1 = *reinterpret_cast<const uint4*>(w + kBlock);
+      const uint32_t ww[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+      uint32_t mine = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mine |= (ww[e] >> nibble(at & 7) & 15u) << nibble(e);
+      const uint16_t* p = cb.v_params + head * kParams + (c >> 3) * (2 * kBlock) + at;
+      v = keys8(mine, p[0] | (uint32_t)p[kBlock] << 16);
+    }
+    out = make_uint4(bf16x2_bits((float)v[0], (float)v[1]), bf16x2_bits((float)v[2], (float)v[3]),
+                     bf16x2_bits((float)v[4], (float)v[5]), bf16x2_bits((float)v[6], (float)v[7]));
+  }
+  const int64_t row = s.row0 + (t - (s.len - s.n));
+  *reinterpret_cast<uint4*>(rows.p + row * rows.row + hk * rows.head + 8 * c) = out;
+}
+
+// ---- attention
+
+// Weights are exp2(score - offset).  The offset is the score of the row's
+// largest less 12, and follows the maximum only where that has outgrown it by
+// more than 3, so that the sums are hardly ever rescaled: weights reach 2^15,
+// and fp16 holds those down to 2^-14, 2^-26 of the largest, in full precision,
+// smaller ones to 2^-24.
+constexpr float kWeightShift = 12.0f, kSlack = 3.0f;
+// A score's exponent is one multiply-add, score factor - offset.  From here on
+// its rounding to fp32 could lift it past fp16's range: there the offset is the
+// rounded score itself and is subtracted from rounded scores.
+constexpr float kLarge = 0x1p23f;
+
+// One workgroup per (rows of one sequence's kv head, split of its blocks).
+// A row is a (new token, query head of the kv head) pair, row i G + g; a wave
+// holds R tiles of 16 rows.
+//
+// Per block of 64 tokens, S^T = K Q^T and O^T += V^T P^T in fp16 MFMAs of
+// 16 x 16 x 32:
+//   - row m of key tile u is token 4 m + u, and a lane's part of the sum over d
+//     is d = 32 g .. 32 g + 31 (lane group g): 16 bytes of a token's codes,
+//     all of one group;
+//   - so lane group g holds the scores of tokens 16 g + 4 r + u, 16 in a row,
+//     which is what P^T wants of it when V^T brings tokens 16 g + 8 h .. in its
+//     step h: a word of codes a lane and row;
+//   - row m of value tile t is d = 8 m + t, so that a lane's rows share a group
+//     and its eight outputs are 16 bytes of a row.
+//
+// Direct: the waves share the rows and take every NW-th block each, reading
+// operands straight from the page (a load instruction covers 1 KiB of keys),
+// and meet in LDS at the end.  Otherwise the waves hold different rows of the
+// same blocks, turn a share of each block into fp16 operands and hand them round
+// through LDS, a block ahead of their use; operand order, 1 KiB an operand, so
+// no access meets a bank twice.
+template <int R, int NW, bool kDirect, int AUX = kCacheDefault>
+__global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnArgs a) {
+  constexpr int kWaveRows = 16 * R, kRows = kDirect ? kWaveRows : NW * kWaveRows;
+  constexpr int KW = kDirect ? NW : 1;  // waves that share the blocks of the same rows
+  constexpr int kPitch = kD + 4;        // floats of a row in the merge
+  constexpr int kStage = 32 * 1024;     // a block's operands
+  constexpr int kMergeBytes = NW * kWaveRows * kPitch * 4;
+  static_assert(kDirect || NW == 4 || NW == 8, "shares of a block's 16 + 16 operands");
+  __shared__ __align__(16) uint8_t lds[kDirect ? kMergeBytes : 2 * kStage];
+  __shared__ float2 l_ml[kDirect ? NW * kWaveRows : 1];
+
+  const Cache4Batch& cb = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int G = a.G, kw = kDirect ? wave : 0, same = kDirect ? 0 : wave;
+  // Workgroups of neighbouring kv heads go to the XCDs in turn, so that all of
+  // a head's row blocks find its pages in one L2.
+  const int hk = blockIdx.x;
+  int split = blockIdx.y, item = blockIdx.z;
+  if ((int)gridDim.y > a.S) {  // more row blocks than one axis of a launch holds
+    item += (split / a.S) * gridDim.z;
+    split %= a.S;
+  }
+
+  // ---- the workgroup's place.  A row's number wg_row0 + x is token i0 + (r0 +
+  // x) / G: one division for the workgroup, and a product for the small numbers
+  // (below 2^13, where the half keeps it clear of the integers by more than its
+  // rounding).
+  const Sequence s =
+      find_sequence(cb, item, [&](int n, int) { return (int)(((uint32_t)(n * G) + kRows - 1) / kRows); });
+  if (s.b < 0) return;
+  const int n_rows = s.n * G, wg_row0 = s.item * kRows, i0 = a.by_g.divide(wg_row0), r0 = wg_row0 - i0 * G;
+  auto token_of = [&](int x) { return i0 + (int)(((float)(r0 + x) + 0.5f) * a.inv_g); };
+  // this split's blocks of those that the workgroup's last row sees
+  const int seen = s.len - s.n + token_of(min(wg_row0 + kRows, n_rows) - 1 - wg_row0) + 1;
+  const int blocks = (max(seen, 0) + kBlock - 1) / kBlock, per = a.by_s.divide(blocks + a.S - 1);
+  const int p_begin = split * per, p_end = min(p_begin + per, blocks);
+  const int p_first = p_begin + kw, rounds = max(p_end - p_first + KW - 1, 0) / KW;  // blocks p_first + KW i < p_end
+
+  // The page of block i, -1: none (past the split's, or out of the pool: tokens that no row sees)
+  typedef const __attribute__((address_space(4))) int32_t* ConstTable;
+  const ConstTable table = (ConstTable)(uintptr_t)(cb.table + (int64_t)s.b * cb.max_blocks);
+  auto page_of = [&](int i) {
+    const int p = p_first + KW * i;
+    const int page = table[max(min(p, p_end - 1), 0)];
+    return p < p_end && page >= 0 && page < cb.n_pages ? page : -1;
+  };
+  int page0 = page_of(0), page1 = page_of(1), page2 = page_of(2);
+
+  // ---- this lane's rows (row l16 of each of the wave's tiles): 32 elements of
+  // each, in fp16 at the row's own power of two, the largest in [2^14, 2^15), so
+  // that elements down to 2^-28 of it are exact
+  f16x8 qf[R][4];
+  float f[R];       // a score's factor, in base-2 units
+  int last_key[R];  // the last token that the row sees, -1 for a row past the end
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    const int x = same * kWaveRows + 16 * t + l16, row = min(x, n_rows - 1 - wg_row0), i = token_of(row);
+    const uint16_t* src = a.q.p + (int64_t)(s.row0 + i) * a.q.row + (int64_t)(hk * G + wg_row0 + row - i * G) * a.q.head + 32 * g;
+    uint32_t w[16], mag = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * e);
+      w[4 * e] = v.x;
+      w[4 * e + 1] = v.y;
+      w[4 * e + 2] = v.z;
+      w[4 * e + 3] = v.w;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mag = absmax_pairs(mag, w[e]);
+    mag = fold_pair_max(mag);
+    mag = __float_as_uint(fold_groups(__uint_as_float(mag), [](float p, float r) { return __uint_as_float(max(__float_as_uint(p), __float_as_uint(r))); }));
+    const int up = min(141 - (int)(mag >> 7), 126);  // mag holds a bf16's bits
+    const float to = __uint_as_float((uint32_t)(127 + up) << 23) * a.q_sign;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      qf[t][e] = __builtin_bit_cast(
+          f16x8, make_uint4(f16x2_bits(bf16_lo(w[4 * e]) * to, bf16_hi(w[4 * e]) * to),
+                            f16x2_bits(bf16_lo(w[4 * e + 1]) * to, bf16_hi(w[4 * e + 1]) * to),
+                            f16x2_bits(bf16_lo(w[4 * e + 2]) * to, bf16_hi(w[4 * e + 2]) * to),
+                            f16x2_bits(bf16_lo(w[4 * e + 3]) * to, bf16_hi(w[4 * e + 3]) * to)));
+    f[t] = fmaxf(__uint_as_float((uint32_t)(127 - up) << 23) * a.scale_log2e, 0x1p-126f);  // above 0: a masked -inf stays
+    last_key[t] = wg_row0 + x < n_rows ? s.len - s.n + i : -1;
+  }
+
+  // ---- a block's codes and parameters as they lie in the page
+  auto bytes = [&](int page, int n) { return page < 0 ? 0u : (uint32_t)n; };  // nothing is read where there is no page
+  auto head_of = [&](int page) { return (int64_t)max(page, 0) * cb.Hkv + hk; };
+  auto rsrc = [&](const void* base, int page, int n) {
+    return make_rsrc(uniform_ptr(static_cast<const uint8_t*>(base) + head_of(page) * n), bytes(page, n));
+  };
+  constexpr int kKeyLoads = kDirect ? 4 : 1, kValueLoads = kDirect ? 4 : 1;
+  // keys: tile u's rows 1 KiB on; a token's params of this lane group's half of d, four tokens 16 bytes
+  const uint32_t k_at = (uint32_t)(l16 * 64 + 16 * g), kp_at = (uint32_t)((g >> 1) * 256 + l16 * 16);
+  // values: step h, half j of a lane's rows
+  const uint32_t v_at = (uint32_t)(g * 1024 + l16 * 16), vp_at = (uint32_t)((l16 >> 3) * 256 + 32 * g);
+  // (not direct) this wave's share: with four waves key tile `wave` and value piece `wave`, with eight
+  // the first four waves' keys, the others' values
+  const bool my_keys = kDirect || NW == 4 || wave < 4, my_values = kDirect || NW == 4 || wave >= 4;
+  const int piece = wave & 3;
+  uint4 kr[kKeyLoads], kp, vr[kValueLoads], vs[kDirect ? 2 : 1], vb[kDirect ? 2 : 1];
+  auto load_keys = [&](int page) {
+    const __amdgpu_buffer_rsrc_t r = rsrc(cb.k_codes, page, kCodeBytes), p = rsrc(cb.k_params, page, kParamBytes);
+    if constexpr (kDirect) {
+      kp = buf_load16<AUX>(p, kp_at);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) kr[u] = buf_load16<AUX>(r, k_at + 1024 * u);
+    } else {
+      kp.x = buf_load4<AUX>(p, kp_at + 4 * piece);
+      kr[0] = buf_load16<AUX>(r, k_at + 1024 * piece);
+    }
+  };
+  auto load_values = [&](int page) {
+    const __amdgpu_buffer_rsrc_t r = rsrc(cb.v_codes, page, kCodeBytes), p = rsrc(cb.v_params, page, kParamBytes);
+    if constexpr (kDirect) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        vs[h] = buf_load16<AUX>(p, vp_at + 16 * h);
+        vb[h] = buf_load16<AUX>(p, vp_at + 128 + 16 * h);
+        vr[2 * h] = buf_load16<AUX>(r, v_at + 512 * h);
+        vr[2 * h + 1] = buf_load16<AUX>(r, v_at + 512 * h + 256);
+      }
+    } else {
+      vs[0] = buf_load16<AUX>(p, vp_at + 16 * (piece >> 1));
+      vb[0] = buf_load16<AUX>(p, vp_at + 128 + 16 * (piece >> 1));
+      vr[0] = buf_load16<AUX>(r, v_at + 256 * piece);
+    }
+  };
+  // Values of tokens that the sequence does not hold are zeros, whatever lies
+  // there: their weights are 0, but 0 times infinity is not.
+  auto clean = [&](uint4& x, int token0) {  // of tokens token0 ..
+    uint32_t* w = &x.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] &= (token0 + 2 * i < s.len ? 0xFFFFu : 0u) | (token0 + 2 * i + 1 < s.len ? 0xFFFF0000u : 0u);
+  };
+  auto clean_values = [&](int i) {
+    const int key0 = (p_first + KW * i) * kBlock;
+    if (key0 + kBlock <= s.len) return;
+#pragma unroll
+    for (int h = 0; h < (kDirect ? 2 : 1); ++h) {
+      const int token0 = key0 + 16 * g + 8 * (kDirect ? h : piece >> 1);
+      clean(vs[h], token0);
+      clean(vb[h], token0);
+    }
+  };
+  auto word = [](const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
+  // (not direct) block i's operands to stage i % 2: keys' (u, step) at 4 u + step, values' (h, t) at 16 + 8 h + t
+  auto stage = [&](int i) {
+    uint8_t* dst = lds + (i & 1) * kStage + lane * 16;
+    if (my_keys) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + (4 * piece + e) * 1024) = keys8(word(kr[0], e), kp.x);
+    }
+    if (my_values) {
+      clean_values(i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + (16 + 4 * piece + e) * 1024) = values8(word(vr[0], e), vs[0], vb[0]);
+    }
+  };
+
+  f32x4 acc[R][8];
+  float m[R], l[R];  // the offset, and the weights' total
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) acc[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  if (my_keys) load_keys(page0);
+  if (my_values) load_values(page0);
+  if constexpr (!kDirect) {
+    stage(0);
+    if (my_keys) load_keys(page1);
+    if (my_values) load_values(page1);
+    lds_barrier();
+  }
+
+  for (int i = 0; i < rounds; ++i) {
+    const int page3 = page_of(i + 3);
+    const int key0 = (p_first + KW * i) * kBlock;
+    const uint8_t* src = lds + (i & 1) * kStage + lane * 16;
+    if constexpr (!kDirect) {  // the other stage was last read before the barrier
+      stage(i + 1);
+      if (my_keys) load_keys(page2);
+      if (my_values) load_values(page2);
+    }
+
+    // ---- scores
+    f32x4 sc[R][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f16x8 kf;
+        if constexpr (kDirect)
+          kf = keys8(word(kr[u], e), word(kp, u));
+        else
+          kf = *reinterpret_cast<const f16x8*>(src + (4 * u + e) * 1024);
+#pragma unroll
+        for (int t = 0; t < R; ++t)
+          sc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][e], e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[t][u], 0, 0, 0);
+      }
+    }
+    if constexpr (kDirect) load_keys(page1);
+
+    // ---- masks and the rows' largest; token 16 g + e is element e / 4 of tile e % 4
+    float x[R][16], top[R];
+    bool all = true;
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][e] = sc[t][e & 3][e >> 2];
+      all = all && last_key[t] >= key0 + kBlock - 1;
+    }
+    if (!__all(all) || page0 < 0) {
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        const int lim = page0 >= 0 ? last_key[t] - key0 - 16 * g : INT_MIN;  // tokens of this lane past it are not seen
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[t][e] = e <= lim ? x[t][e] : -INFINITY;
+      }
+    }
+    bool outgrown = false;
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      top[t] = x[t][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top[t] = fmaxf(top[t], x[t][e]);
+      top[t] = fold_groups(top[t], [](float p, float r) { return fmaxf(p, r); }) * f[t];
+      top[t] = fabsf(top[t]) >= kLarge ? top[t] : top[t] - kWeightShift;  // the offset that it asks for
+      outgrown = outgrown || top[t] - m[t] > kSlack;
+    }
+    if (__any(outgrown)) {
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        // a row's own maximum alone moves its offset: its result does not
+        // depend on the rows that share the wave
+        const bool up = top[t] - m[t] > kSlack;
+        const float alpha = up ? __builtin_amdgcn_exp2f(m[t] - top[t]) : 1.0f;
+        m[t] = up ? top[t] : m[t];
+        l[t] *= alpha;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
+      }
+    }
+
+    // ---- weights
+    f16x8 pw[R][2];
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      const bool none = m[t] == -INFINITY;
+      float by = f[t], off = none ? 0.0f : -m[t];
+      if (__builtin_expect(__any(fabsf(off) >= kLarge - 16.0f), 0)) {
+        const bool large = fabsf(off) >= kLarge - 16.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[t][e] = large ? x[t][e] * by : x[t][e];
+        by = large ? 1.0f : by;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], by, off));
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        pw[t][h] = __builtin_bit_cast(
+            f16x8, make_uint4(f16x2_bits(x[t][8 * h], x[t][8 * h + 1]), f16x2_bits(x[t][8 * h + 2], x[t][8 * h + 3]),
+                              f16x2_bits(x[t][8 * h + 4], x[t][8 * h + 5]), f16x2_bits(x[t][8 * h + 6], x[t][8 * h + 7])));
+      float sum[4] = {x[t][0], x[t][1], x[t][2], x[t][3]};
+#pragma unroll
+      for (int e = 4; e < 16; ++e) sum[e & 3] += x[t][e];
+      l[t] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+
+    // ---- O^T += V^T P^T
+    if constexpr (kDirect) clean_values(i);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        f16x8 vf;
+        if constexpr (kDirect)
+          vf = values8(word(vr[2 * h + d / 4], d % 4), vs[h], vb[h]);
+        else
+          vf = *reinterpret_cast<const f16x8*>(src + (16 + 8 * h + d) * 1024);
+#pragma unroll
+        for (int t = 0; t < R; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pw[t][h], acc[t][d], 0, 0, 0);
+      }
+    if constexpr (kDirect)
+      load_values(page1);
+    else
+      lds_barrier();
+    page0 = page1;
+    page1 = page2;
+    page2 = page3;
+  }
+#pragma unroll
+  for (int t = 0; t < R; ++t) l[t] = fold_groups(l[t], [](float p, float r) { return p + r; }) * kTotalUnit;
+
+  // Where a row's result goes: its partial sums, or the output.
+  auto write8 = [&](int row, int d, const float (&o)[8], float mx, float lsum) {
+    const int i = token_of(row - wg_row0), h = hk * G + row - i * G;
+    const int64_t tok = s.row0 + i;
+    if (a.S > 1) {
+      const int64_t at = ((int64_t)split * cb.T + tok) * a.H + h;
+      float* po = a.part_o + at * kD + d;
+      *reinterpret_cast<float4*>(po) = make_float4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<float4*>(po + 4) = make_float4(o[4], o[5], o[6], o[7]);
+      if (d == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(mx, lsum);
+    } else {
+      *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + h * a.o.head + d) = output8(o, lsum);
+    }
+  };
+  if constexpr (kDirect) {
+    // the waves' partial results of the same rows meet in LDS
+    float* l_o = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      const int r = wave * kWaveRows + 16 * t + l16;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int d = 0; d < 8; d += 4)
+          *reinterpret_cast<float4*>(&l_o[r * kPitch + 32 * g + 8 * e + d]) =
+              make_float4(acc[t][d][e], acc[t][d + 1][e], acc[t][d + 2][e], acc[t][d + 3][e]);
+      if (g == 0) l_ml[r] = make_float2(m[t], l[t]);
+    }
+    lds_barrier();
+    for (int i = tid; i < kRows * 16; i += NW * 64) {
+      const int r = i >> 4, d = (i & 15) * 8, row = wg_row0 + r;  // row r lies r + kRows w rows from the first wave's
+      if (row >= n_rows) continue;
+      float mx = -INFINITY, lsum = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) mx = fmaxf(mx, l_ml[r + w * kRows].x);
+      const float base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float2 ml = l_ml[r + w * kRows];
+        const float by = __builtin_amdgcn_exp2f(ml.x - base);
+        lsum = fmaf(ml.y, by, lsum);
+        const float* p = &l_o[(r + w * kRows) * kPitch + d];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(p[e], by, o[e]);
+      }
+      write8(row, d, o, mx, lsum);
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      const int row = wg_row0 + same * kWaveRows + 16 * t + l16;
+      if (row >= n_rows) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float o[8];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) o[d] = acc[t][d][e];
+        write8(row, 32 * g + 8 * e, o, m[t], l[t]);
+      }
+    }
+  }
+}
+
+// The forms of a call, and what one of its workgroups costs in ns: alone on a
+// CU lat + lat_round a round (a block of each of the KW waves that share one);
+// in a full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
+// thr_round a round.
+typedef void (*Attn4Fn)(const Cache4AttnArgs);
+struct Attn4Form {
+  int rows, KW, threads;
+  int64_t lat, lat_round, thr, thr_round;
+  Attn4Fn fn;
+};
+const Attn4Form kForms[] = {
+    {16, 4, 256, 800, 970, 860, 700, cache4_attention<1, 4, true>},
+    {64, 1, 256, 1570, 1010, 1840, 720, cache4_attention<1, 4, false>},
+    {128, 1, 256, 3010, 1200, 4000, 1200, cache4_attention<2, 4, false>},
+};
+const Attn4Fn kStreamFn = cache4_attention<1, 4, true, kCacheStream>;
+constexpr int64_t kTokenBytes = kD + 16;  // of a kv head's keys and values
+// A cache that is read once and is larger than this does not stay in the
+// memory-side cache (256 MB) until the next call: it is read past it.
+constexpr int64_t kStreamBytes = int64_t(160) << 20;
+constexpr int64_t kMaxAxis = 65535;  // workgroups along the second and third axis of a launch
+
+struct Attn4Plan {
+  int form = 0, S = 1;
+  bool stream = false;
+  int64_t tiles = 0;  // the most row blocks that the batch can have
+};
+
+Attn4Plan plan_attention(int B, int T, int H, int Hkv, int max_len) {
+  const int64_t G = H / Hkv, n = (T + B - 1) / B, blocks = (max_len + kBlock - 1) / kBlock;
+  const int64_t most = (int64_t)T * H <= (1 << 22) ? blocks : 1;  // splits
+  constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  Attn4Plan p;
+  int64_t least = INT64_MAX;
+  for (int f = 0; f < (int)(sizeof kForms / sizeof kForms[0]); ++f) {
+    const Attn4Form& k = kForms[f];
+    const int by_rows = __builtin_ctz(k.rows), by_kw = __builtin_ctz(k.KW);
+    const int64_t tiles = B * ((n * G + k.rows - 1) >> by_rows) * Hkv;
+#pragma unroll
+    for (int S : kSplits) {
+      if (S > 1 && S > most) break;
+      const int64_t rounds = ((uint64_t)(blocks + S - 1) / S + k.KW - 1) >> by_kw;
+      const int64_t cost = std::max(k.lat + rounds * k.lat_round, ((tiles * S + 255) >> 8) * (k.thr + rounds * k.thr_round)) +
+                           (S > 1 ? 1820 + (int64_t)((uint64_t)S * T * H * 21 / 100) : 0);
+      if (cost < least) {
+        least = cost;
+        p.form = f;
+        p.S = S;
+      }
+    }
+  }
+  const int64_t rows = kForms[p.form].rows;
+  // every sequence's last row block may be partial, but each has a row
+  p.tiles = std::min<int64_t>(T * G / rows + B, T * ((G + rows - 1) / rows));
+  p.stream = p.form == 0 && n * G <= rows && (int64_t)B * max_len >= kStreamBytes / kTokenBytes / Hkv;
+  return p;
+}
+
+size_t workspace_of(const Attn4Plan& p, int T, int H) {
+  return p.S > 1 ? kCounterRegionBytes + (size_t)p.S * T * H * (kD + 2) * sizeof(float) : 0;
+}
+
+// Groups of eight tokens that a batch's rows touch at most: (n + 14) / 8 of a
+// sequence with n rows, and no more than its rows.
+unsigned most_eights(const Cache4Batch& c) {
+  return (unsigned)std::min<int64_t>(c.T, ((int64_t)c.T + 14ll * std::min(c.B, c.T)) / kEight);
+}
+
+}  // namespace
+
+hipError_t launch_cache4_append(const Cache4RowsArgs& a, hipStream_t stream) {
+  cache4_append<<<dim3(most_eights(a.c), (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache4_read(const Cache4RowsArgs& a, hipStream_t stream) {
+  cache4_read<<<dim3(most_eights(a.c), (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+size_t cache4_attention_workspace(int B, int T, int H, int Hkv, int max_len) {
+  return workspace_of(plan_attention(B, T, H, Hkv, max_len), T, H);
+}
+
+bool launch_cache4_attention(const Cache4AttnArgs& a0, void* workspace, size_t bytes, hipStream_t stream, hipError_t& error) {
+  Cache4AttnArgs a = a0;
+  const Attn4Plan p = plan_attention(a.c.B, a.c.T, a.H, a.c.Hkv, a.max_len);
+  const size_t need = workspace_of(p, a.c.T, a.H);
+  if (need && (bytes < need || !workspace || (uintptr_t)workspace % 256)) return false;
+  a.G = a.H / a.c.Hkv;
+  a.S = p.S;
+  a.inv_g = 1.0f / (float)a.G;
+  a.by_g = Divisor(a.G);
+  a.by_s = Divisor(a.S);
+  if (a.S > 1) {
+    a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCounterRegionBytes);
+    a.part_ml = a.part_o + (size_t)a.S * a.c.T * a.H * kD;
+  }
+  const Attn4Form& k = kForms[p.form];
+  const unsigned z = (unsigned)std::min<int64_t>(p.tiles, kMaxAxis), y = (unsigned)((p.tiles + z - 1) / z) * (unsigned)a.S;
+  (p.stream ? kStreamFn : k.fn)<<<dim3((unsigned)a.c.Hkv, y, z), dim3(k.threads), 0, stream>>>(a);
+  if (a.S > 1) {
+    const int P = a.S <= 16 ? 4 : 16;
+    const int64_t threads = (int64_t)a.c.T * a.H * (kD / 8) * P;
+    const Attn4Fn merge = P == 4 ? cache_attention_merge<4, Cache4AttnArgs> : cache_attention_merge<16, Cache4AttnArgs>;
+    merge<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream>>>(a);
+  }
+  error = hipGetLastError();
+  return true;
+}
+
+}  // namespace w4a8
