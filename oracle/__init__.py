@@ -333,6 +333,61 @@ def cache_attention(q_bits, pos, k, v, cos_t, sin_t, scale, first):
     return o, bnd, np.abs(q).max(axis=-1), top
 
 
+def qk_norm_rope(x_bits, gamma_bits, eps, pos, axis, cos_t, sin_t):
+    """RMSNorm (gain gamma_bits [128], None: no norm) of heads x_bits [T][H][128]
+    (bf16 bits) and their rotation at pos [axes][T] (None: no rotation), pair i
+    by axis[i], in fp64 on the fp32 tables.  Returns (y fp64, the sums of the
+    magnitudes of the rotation's two terms, which bound fp32's error)."""
+    h = _f32(np.asarray(x_bits, np.uint16)).astype(np.float64)
+    if gamma_bits is not None:
+        h = h / np.sqrt((h * h).mean(-1, keepdims=True) + eps) * _f32(np.asarray(gamma_bits, np.uint16)).astype(np.float64)
+    if pos is None:
+        return h, np.abs(h)
+    at = np.clip(np.asarray(pos)[np.asarray(axis)], 0, len(cos_t) - 1).T  # [T][64]
+    c, s = (t[at, np.arange(64)].astype(np.float64)[:, None] for t in (cos_t, sin_t))
+    a, b = h[..., :64], h[..., 64:]
+    return (np.concatenate([a * c - b * s, b * c + a * s], -1),
+            np.concatenate([np.abs(a * c) + np.abs(b * s), np.abs(b * c) + np.abs(a * s)], -1))
+
+
+def cache4_quantize(x_bits):
+    """The 4-bit cache's codes of vectors x_bits [..][128] (bf16 bits): codes
+    uint8 [..][128], scales and offsets fp16 [..][2] of the groups of 64.  Every
+    step one fp32 IEEE operation; NaN counts as 0, magnitudes above 2^14 as 2^14."""
+    x = _f32(np.asarray(x_bits, np.uint16))
+    x = np.clip(np.where(np.isnan(x), np.float32(0), x), np.float32(-16384), np.float32(16384))
+    x = x.reshape(*x.shape[:-1], 2, 64)
+    lo, hi = x.min(-1), x.max(-1)
+    s = ((hi - lo) / np.float32(15)).astype(np.float16)
+    s32 = s.astype(np.float32)
+    b = (lo - np.float32(16) * s32).astype(np.float16)
+    t = (x - b.astype(np.float32)[..., None]) / np.where(s32 > 0, s32, np.float32(1))[..., None] - np.float32(16)
+    codes = np.where(s32[..., None] > 0, np.clip(np.rint(t), 0, 15), 0).astype(np.uint8)
+    return codes.reshape(*codes.shape[:-2], 128), s, b
+
+
+def cache4_values(codes, s, b):
+    """What the codes stand for: fp16(s (16 + code) + b), rounded once, as fp64."""
+    c = np.asarray(codes).reshape(*codes.shape[:-1], 2, 64).astype(np.float64)
+    v = s.astype(np.float64)[..., None] * (16 + c) + b.astype(np.float64)[..., None]  # exact in fp64
+    return v.astype(np.float16).astype(np.float64).reshape(codes.shape)
+
+
+def cache4_codes(words, values):
+    """The codes of a page's head, uint8 [64][128] (token by d), from its words:
+    keys' [4][16][16] or values' [8][2][16][4]."""
+    words = np.asarray(words).view(np.uint32).reshape(-1)
+    out = np.empty((64, 128), np.uint8)
+    for t in range(64):
+        for d in range(128):
+            if values:
+                at, e = ((t // 8 * 2 + d // 4 % 2) * 16 + d // 8) * 4 + d % 4, t % 8
+            else:
+                at, e = (t % 4 * 16 + t // 4) * 16 + d // 8, d % 8
+            out[t, d] = int(words[at]) >> (4 * (e // 2) + 16 * (e % 2)) & 15
+    return out
+
+
 def rope_tables(P, D, base=10000.0):
     """fp32 cos / sin tables [P][D/2] for angle p * base^(-2i/D), from fp64."""
     i = np.arange(D // 2, dtype=np.float64)

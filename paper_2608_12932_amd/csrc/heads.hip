@@ -77,14 +77,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope(const QkNormRopeArgs a) {
     }
     const uint16_t* gamma = k ? a.k.gamma : a.q.gamma;
     if (gamma) {  // (both heads' kinds may share a wave, of which one has no norm)
-      float ss = 0.0f;
+      float ss = 0.0f;  // of x^2 / 128, which is finite where the mean is
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+      for (int e = 0; e < 8; ++e) ss = fmaf(x[e] * (1.0f / kD), x[e], fmaf(y[e] * (1.0f / kD), y[e], ss));
       auto add = [&](auto ctrl) { ss += __uint_as_float(lane_move<decltype(ctrl)::value>(__float_as_uint(ss))); };
       add(std::integral_constant<int, kXor1>{});  // over the head's 8 lanes
       add(std::integral_constant<int, kXor2>{});
       add(std::integral_constant<int, kMirror8>{});
-      const float r = 1.0f / sqrtf(ss * (1.0f / kD) + a.eps);
+      const float r = 1.0f / sqrtf(ss + a.eps);
       const uint4 g0 = *reinterpret_cast<const uint4*>(gamma + 8 * c), g1 = *reinterpret_cast<const uint4*>(gamma + kHalf + 8 * c);
       const uint32_t w0[4] = {g0.x, g0.y, g0.z, g0.w}, w1[4] = {g1.x, g1.y, g1.z, g1.w};
 #pragma unroll

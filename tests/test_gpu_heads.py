@@ -1,0 +1,221 @@
+"""w4a8_qk_norm_rope against the oracle in fp64.
+
+Tolerance, derived.  The sum of squares adds positive terms in fp32: 16 by
+multiply-adds and 3 lane folds, within 19 steps of 2^-24; mean, eps, square root
+and division: the factor r within (19 / 2 + 4) 2^-24; two products with it, the
+rotation's product and its sum 4 more.  So an element is off by at most 18 2^-24
+of the two terms' magnitudes M, and then rounded to bf16, half a step, 2^-8 of
+itself: |y - y64| <= 2^-8 |y64| + (1 + 2^-8) 2^-19 M.  bf16's least normal number
+is fp32's: below it a step is 2^-133."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2608_12932_amd as w
+from paper_2608_12932_amd import inputs as I
+from helpers import bf16_dev, dev, to_np_bits
+
+pytestmark = pytest.mark.gpu
+
+D, EPS = 128, 1e-6
+
+
+def bits(rng, *shape, spread=0.5):
+    return I.to_bf16_bits((rng.standard_normal(shape) * np.exp(spread * rng.standard_normal(shape[1:]))).astype(np.float32))
+
+
+def close(got, x, gamma, eps, pos, axis, tables, label=""):
+    y, mag = oracle.qk_norm_rope(x, gamma, eps, pos, axis, *tables)
+    g = oracle._f32(to_np_bits(got.contiguous())).astype(np.float64)
+    bad = np.abs(g - y) > 2.0 ** -8 * np.abs(y) + (1 + 2.0 ** -8) * 2.0 ** -19 * mag + 2.0 ** -134
+    assert not bad.any(), (label, np.argwhere(bad)[:4], g[bad][:4], y[bad][:4])
+
+
+class Case:
+    def __init__(self, T, H, Hkv, axes=None, seed=0, n_pos=300):
+        rng = self.rng = np.random.Generator(np.random.PCG64(seed))
+        self.T, self.H, self.Hkv = T, H, Hkv
+        self.axes = axes
+        self.axis = np.frombuffer(axes, np.uint8) if axes else np.zeros(64, int)
+        self.qkv = bits(rng, T, H + 2 * Hkv, D)
+        self.g = [bits(rng, D, spread=0), bits(rng, D, spread=0)]
+        A = int(self.axis.max()) + 1
+        self.pos = rng.integers(-2, n_pos + 2, (A, T)).astype(np.int32)
+        self.tables = oracle.rope_tables(n_pos, D)
+        self.dev = bf16_dev(self.qkv)
+        self.dpos = torch.from_numpy(self.pos).to(dev())
+        self.dt = [torch.from_numpy(t).to(dev()) for t in self.tables]
+        self.dg = [bf16_dev(g) for g in self.g]
+
+    def views(self, m=None):
+        m = self.dev if m is None else m
+        return m[:, :self.H], m[:, self.H:self.H + self.Hkv]
+
+    def run(self, **kw):
+        q, k = self.views()
+        a = dict(q=q, k=k, gamma_q=self.dg[0], gamma_k=self.dg[1], eps=EPS, pos=self.dpos if self.axes else self.dpos[0], rope_cos=self.dt[0],
+                 rope_sin=self.dt[1], axes=self.axes)
+        a.update(kw)
+        return w.w4a8_qk_norm_rope(**a)
+
+    def check(self, q, k, norm=True, rotate=True, label=""):
+        pos = self.pos if rotate else None
+        if q is not None:
+            close(q, self.qkv[:, :self.H], self.g[0] if norm else None, EPS, pos, self.axis, self.tables, label + " q")
+        if k is not None:
+            close(k, self.qkv[:, self.H:self.H + self.Hkv], self.g[1] if norm else None, EPS, pos, self.axis, self.tables, label + " k")
+
+
+AXES = [None, w.rope_axes((16, 24, 24)), w.rope_axes((24, 20, 20), True), w.rope_axes((31, 7, 13, 13)), w.rope_axes((32, 32))]
+
+
+@pytest.mark.parametrize("axes", range(len(AXES)))
+@pytest.mark.parametrize("T,H,Hkv", [(1, 32, 8), (1, 1, 1), (3, 28, 4), (129, 7, 3), (1100, 32, 8), (2500, 8, 1), (1030, 40, 8), (2100, 13, 2)])
+def test_against_the_oracle(T, H, Hkv, axes):
+    print(f"[case] norm+rope T={T} H={H} Hkv={Hkv} axes={axes}", flush=True)
+    c = Case(T, H, Hkv, AXES[axes], seed=T + axes)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("T", [2, 1500])
+def test_without_a_norm_or_a_rotation(T):
+    c = Case(T, 12, 4, AXES[2], seed=3)
+    c.check(*c.run(gamma_q=None, gamma_k=None), norm=False)
+    c.check(*c.run(pos=None, rope_cos=None, rope_sin=None, axes=None), rotate=False)
+    q, k = c.run(gamma_k=None)  # one kind with a norm, the other without, in waves that hold both
+    c.check(q, None)
+    c.check(None, k, norm=False)
+    q, k = c.run(q=None, gamma_q=None)
+    assert q is None
+    c.check(None, k)
+    q, k = c.run(k=None, gamma_k=None)
+    assert k is None
+    c.check(q, None)
+
+
+def test_in_place_and_strided_outputs():
+    c = Case(70, 12, 4, AXES[1], seed=4)
+    want = c.run()
+    m = c.dev.clone()
+    q, k = c.views(m)
+    got = c.run(q=q, k=k, q_out=q, k_out=k)
+    assert got[0] is q and got[1] is k
+    for a, b in zip((q, k), want):
+        assert torch.equal(a, b)
+    assert torch.equal(m[:, 16:], c.dev[:, 16:])  # the values' columns are left alone
+    # into the columns of another matrix, and head by head ([H][T][128], transposed)
+    big = torch.full((70, 20, D), 7.0, dtype=torch.bfloat16, device=dev())
+    kt = torch.full((4, 72, D), 7.0, dtype=torch.bfloat16, device=dev())
+    c.run(q_out=big[:, 2:14], k_out=kt[:, 1:71].transpose(0, 1))
+    assert torch.equal(big[:, 2:14], want[0]) and torch.equal(kt[:, 1:71].transpose(0, 1), want[1])
+    assert (big[:, :2] == 7).all() and (big[:, 14:] == 7).all() and (kt[:, 0] == 7).all() and (kt[:, 71] == 7).all()
+    # into the values' columns of the same matrix: no element is shared
+    m = c.dev.clone()
+    q, k = c.views(m)
+    c.run(q=q, k=k, k_out=m[:, 16:])
+    assert torch.equal(m[:, 16:], want[1]) and torch.equal(m[:, :16], c.dev[:, :16])
+    # head-major inputs
+    q, k = c.views()
+    got = c.run(q=q.transpose(0, 1).contiguous().transpose(0, 1), k=k.contiguous())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_special_heads():
+    c = Case(4, 4, 2, AXES[0], seed=5)
+    x = c.qkv
+    x[0, 0] = 0          # zeros: eps alone under the root
+    x[0, 1] = 0x0100     # tiny
+    x[1, 0] = 0x5E00     # large: 2^61, its square is finite
+    x[1, 1, 3] = 0x7FC0  # NaN stays within its head
+    x[2, 2, 5] = 0x7F80  # so does infinity
+    c.dev = bf16_dev(x)
+    q, k = c.run()
+    assert torch.isnan(q[1, 1]).all() and torch.isnan(q[2, 2]).any()
+    keep = np.ones((4, 4), bool)
+    keep[1, 1] = keep[2, 2] = False
+    y, mag = oracle.qk_norm_rope(np.where(keep[..., None], x[:, :4], 0), c.g[0], EPS, c.pos, c.axis, *c.tables)
+    got = oracle._f32(to_np_bits(q)).astype(np.float64)
+    assert (np.abs(got - y)[keep] <= (2.0 ** -8 * np.abs(y) + (1 + 2.0 ** -8) * 2.0 ** -19 * mag + 2.0 ** -134)[keep]).all()
+    c.check(None, k)
+
+
+def test_largest_rows_past_32_bit_offsets():
+    # a matrix of more than 2^31 elements, of which the last rows' heads are used
+    T, row = 4100, 526336  # elements: 2.16e9
+    m = torch.empty(T * row, dtype=torch.bfloat16, device=dev())
+    c = Case(T, 3, 1, AXES[0], seed=6)
+    q = m.view(T, row)[:, :3 * D].unflatten(1, (3, D))
+    k = m.view(T, row)[:, -D:].unflatten(1, (1, D))
+    q.copy_(c.dev[:, :3])
+    k.copy_(c.dev[:, 3:4])
+    want = c.run()
+    got = c.run(q=q, k=k, q_out=q, k_out=k)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_stream_and_graph():
+    c = Case(33, 32, 8, AXES[2], seed=7)
+    want = c.run()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = c.run(stream=s)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    outs = [torch.empty_like(t) for t in want]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.run(q_out=outs[0], k_out=outs[1])
+    for step in range(3):
+        c.dpos.add_(1)
+        c.dev.mul_(-1)
+        g.replay()
+        want = c.run()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1]), step
+
+
+def test_native_path_takes_the_plain_call(monkeypatch):
+    c = Case(5, 4, 2, AXES[1], seed=8)
+    seen = []
+    real = w._load_fast()
+
+    class Spy:
+        def __getattr__(self, name):
+            def call(*a):
+                r = getattr(real, name)(*a)
+                seen.append(r is not None)
+                return r
+            return call
+
+    monkeypatch.setattr(w, "_fast", Spy())
+    c.run()
+    c.run(pos=c.dpos)
+    assert seen == [True, True]
+    c.run(eps=1)  # an integer: the interpreted path
+    assert seen == [True, True, False]
+
+
+def test_refusals():
+    c = Case(6, 4, 2, AXES[1], seed=9)
+    q, k = c.views()
+    for kw, err in ((dict(q=q.float()), TypeError), (dict(q=q[..., :64]), ValueError), (dict(k=k[:5]), ValueError), (dict(gamma_q=c.dg[0][:64]), ValueError),
+                    (dict(gamma_k=c.dg[0].float()), TypeError), (dict(pos=c.dpos.long()), TypeError), (dict(pos=c.dpos[:, :5]), ValueError),
+                    (dict(axes=b"\0" * 63), ValueError), (dict(axes=b"\3" * 64), w.W4A8Error), (dict(q_out=q[:, :3]), ValueError),
+                    (dict(eps=0.0), w.W4A8Error), (dict(k_out=q[:, :2]), w.W4A8Error), (dict(q_out=q.flip(0)[:, :4].expand(6, 4, D)[:, [0, 0, 0, 0]].float()), TypeError),
+                    (dict(q=q.transpose(1, 2).contiguous().transpose(1, 2)), ValueError), (dict(rope_cos=c.dt[0][:, :32]), ValueError),
+                    (dict(q_out=c.dev[:1, :4].expand(6, 4, D)), w.W4A8Error), (dict(q=q.cpu()), TypeError), (dict(k=k.cpu()), TypeError),
+                    (dict(gamma_q=None, gamma_k=None, pos=None, rope_cos=None, rope_sin=None, axes=None), w.W4A8Error)):
+        with pytest.raises(err):
+            c.run(**kw)
+    c.check(*c.run())
+
+
+def test_empty():
+    c = Case(4, 4, 2, AXES[1], seed=10)
+    q, k = c.views()
+    got = c.run(q=q[:0], k=k[:0], pos=c.dpos[:, :0].contiguous())
+    assert got[0].shape == (0, 4, D) and got[1].shape == (0, 2, D)
+    got = c.run(k=k[:, :0])
+    assert got[1].shape == (4, 0, D)
+    c.check(got[0], None)
