@@ -540,13 +540,11 @@ w4a8_status w4a8_qk_norm_rope(const w4a8_heads* q, const w4a8_heads* k, int64_t 
   QkNormRopeArgs a{};
   if (rope) {
     if (rope->n_axes < 1 || rope->n_axes > 4 || rope->n_pos < 1 || rope->n_pos > (int64_t(1) << 30)) return W4A8_EINVAL;
-    a.whole = true;
     for (int i = 0; rope->axis && i < kCacheD / 2; ++i) {
       const uint64_t x = rope->axis[i];
       if ((int64_t)x >= rope->n_axes) return W4A8_EINVAL;
       a.axis_lo |= (x & 1) << i;
       a.axis_hi |= (x >> 1) << i;
-      a.whole = a.whole && x == rope->axis[i & ~7];
     }
   }
   if (T == 0 || (!kinds[0] && !kinds[1])) return W4A8_OK;

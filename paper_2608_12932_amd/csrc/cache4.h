@@ -64,7 +64,6 @@ struct QkNormRopeArgs {
   const float* rope_sin;
   int n_pos, axes;
   uint64_t axis_lo, axis_hi;  // bits 0 and 1 of each pair's axis
-  bool whole;             // the eight pairs of a lane share an axis
 };
 hipError_t launch_qk_norm_rope(const QkNormRopeArgs& a, hipStream_t stream);
 
