@@ -32,9 +32,11 @@ __device__ __forceinline__ f16x2 as_f16x2(uint32_t u) { return __builtin_bit_cas
 // Eight values from a word: element 2 i in bits 4 i .., element 2 i + 1 in bits
 // 16 + 4 i ..; s[i] and b[i] are the scales and offsets of elements 2 i, 2 i + 1.
 __device__ __forceinline__ f16x8 values8(uint32_t w, const f16x2 (&s)[4], const f16x2 (&b)[4]) {
-  constexpr uint32_t kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;
-  const uint32_t f[4] = {((w << 6) & kMask) | kSixteen, ((w << 2) & kMask) | kSixteen, ((w >> 2) & kMask) | kSixteen,
-                         ((w >> 6) & kMask) | kSixteen};
+  uint32_t mask = 0x03C003C0u, sixteen = 0x4C004C00u;
+  asm("" : "+s"(mask));  // in registers: as literals they cannot share the instruction that masks and inserts
+  asm("" : "+v"(sixteen));
+  const uint32_t f[4] = {((w << 6) & mask) | sixteen, ((w << 2) & mask) | sixteen, ((w >> 2) & mask) | sixteen,
+                         ((w >> 6) & mask) | sixteen};
   uint4 r;
   r.x = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_f16x2(f[0]), s[0], b[0]));
   r.y = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_f16x2(f[1]), s[1], b[1]));
@@ -56,11 +58,12 @@ __device__ __forceinline__ f16x8 values8(uint32_t w, const uint4& s4, const uint
 }
 __device__ __forceinline__ int nibble(int e) { return 4 * (e >> 1) + 16 * (e & 1); }  // bits of element e
 
-// Items of append and read: the aligned groups of eight tokens that a
-// sequence's last n tokens touch.
+// The aligned groups of Size tokens that a sequence's last n tokens touch: the
+// items of append (eight tokens, those of a word of values) and read (blocks).
 constexpr int kEight = 8;
-__device__ __forceinline__ int eights(int n, int len) {
-  return n > 0 && len > 0 ? (len - 1) / kEight - max(len - n, 0) / kEight + 1 : 0;
+template <int Size>
+__device__ __forceinline__ int touched(int n, int len) {
+  return n > 0 && len > 0 ? (len - 1) / Size - max(len - n, 0) / Size + 1 : 0;
 }
 
 // ---- append
@@ -73,7 +76,7 @@ __global__ __launch_bounds__(256) void cache4_append(const Cache4RowsArgs a) {
   const Cache4Batch& cb = a.c;
   const int tid = threadIdx.x & 127, hk = blockIdx.y;
   const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7) == 0;
-  const Sequence s = find_sequence(cb, blockIdx.x, [](int n, int len) { return eights(n, len); });
+  const Sequence s = find_sequence(cb, blockIdx.x, [](int n, int len) { return touched<kEight>(n, len); });
   if (s.b < 0) return;
   const int first = max(s.len - s.n, 0);  // the first new token that has a place
   const int t8 = first / kEight + s.item, page = cb.table[(int64_t)s.b * cb.max_blocks + t8 / (kBlock / kEight)];
@@ -151,43 +154,58 @@ __global__ __launch_bounds__(256) void cache4_append(const Cache4RowsArgs a) {
 
 // ---- read
 
-// One workgroup per (eight tokens, kv head), 16 threads to a token's keys or
-// values.  The eight tokens of a word of values are eight threads' that read
-// it each, from the first cache.
+// One workgroup per (block, kv head): half of its threads take the keys, half
+// the values, eight elements of eight tokens each: a word of either is eight
+// tokens' (values) or one token's (keys).  So every code is read once, and a
+// thread has all of its loads in flight together.
 __global__ __launch_bounds__(256) void cache4_read(const Cache4RowsArgs a) {
   const Cache4Batch& cb = a.c;
   const int tid = threadIdx.x & 127, hk = blockIdx.y;
   const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7) == 0;
   const TokenRows rows = keys ? a.k : a.v;
   if (!rows.p) return;
-  const Sequence s = find_sequence(cb, blockIdx.x, [](int n, int len) { return eights(n, len); });
+  const Sequence s = find_sequence(cb, blockIdx.x, [](int n, int len) { return touched<kBlock>(n, len); });
   if (s.b < 0) return;
-  const int first = max(s.len - s.n, 0), t8 = first / kEight + s.item;
-  const int page = cb.table[(int64_t)s.b * cb.max_blocks + t8 / (kBlock / kEight)];
-  const int c = tid & 15, t = t8 * kEight + (tid >> 4), at = t & (kBlock - 1);
-  if (t < first || t >= s.len) return;
-  uint4 out = make_uint4(0u, 0u, 0u, 0u);
-  if (page >= 0 && page < cb.n_pages) {
-    const int64_t head = (int64_t)page * cb.Hkv + hk;
-    f16x8 v;
-    if (keys) {
-      v = keys8(cb.k_codes[head * kCodeWords + ((at & 3) * 16 + (at >> 2)) * 16 + c],
-                reinterpret_cast<const uint32_t*>(cb.k_params)[head * (kParams / 2) + (c >> 3) * kBlock + at]);
-    } else {
-      const uint32_t* w = cb.v_codes + head * kCodeWords + (t8 & 7) * kD + 4 * c;
-      const uint4 w0 = *reinterpret_cast<const uint4*>(w), w1 = *reinterpret_cast<const uint4*>(w + kBlock);
-      const uint32_t ww[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-      uint32_t mine = 0;
+  const int first = max(s.len - s.n, 0), blk = first / kBlock + s.item;
+  const int page = cb.table[(int64_t)s.b * cb.max_blocks + blk];
+  const int c = tid & 15, t8 = tid >> 4, t0 = blk * kBlock + t8 * kEight;
+  const bool held = page >= 0 && page < cb.n_pages;
+  const int64_t head = (int64_t)(held ? page : 0) * cb.Hkv + hk;
+  uint32_t out[8][4];  // eight elements of each token, as bf16
+  if (keys) {
+    const uint32_t* w = cb.k_codes + head * kCodeWords + 2 * t8 * 16 + c;  // tokens 8 t8 + 4 i + j in rows 16 j + 2 t8 + i
+    const uint4* p = reinterpret_cast<const uint4*>(cb.k_params + head * kParams + (c >> 3) * (2 * kBlock) + 16 * t8);
+    const uint4 p0 = p[0], p1 = p[1];
+    const uint32_t sb[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+    uint32_t code[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mine |= (ww[e] >> nibble(at & 7) & 15u) << nibble(e);
-      const uint16_t* p = cb.v_params + head * kParams + (c >> 3) * (2 * kBlock) + at;
-      v = keys8(mine, p[0] | (uint32_t)p[kBlock] << 16);
+    for (int e = 0; e < 8; ++e) code[e] = w[((e & 3) * 16 + (e >> 2)) * 16];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const f16x8 v = keys8(code[e], sb[e]);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) out[e][d] = bf16x2_bits((float)v[2 * d], (float)v[2 * d + 1]);
     }
-    out = make_uint4(bf16x2_bits((float)v[0], (float)v[1]), bf16x2_bits((float)v[2], (float)v[3]),
-                     bf16x2_bits((float)v[4], (float)v[5]), bf16x2_bits((float)v[6], (float)v[7]));
+  } else {
+    const uint32_t* w = cb.v_codes + head * kCodeWords + t8 * kD + 4 * c;
+    const uint4 w0 = *reinterpret_cast<const uint4*>(w), w1 = *reinterpret_cast<const uint4*>(w + kBlock);
+    const uint4* p = reinterpret_cast<const uint4*>(cb.v_params + head * kParams + (c >> 3) * (2 * kBlock) + 8 * t8);
+    const uint4 s4 = p[0], b4 = p[kBlock / 8];
+    const uint32_t ww[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const f16x8 x = values8(ww[2 * d], s4, b4), y = values8(ww[2 * d + 1], s4, b4);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e][d] = bf16x2_bits((float)x[e], (float)y[e]);
+    }
   }
-  const int64_t row = s.row0 + (t - (s.len - s.n));
-  *reinterpret_cast<uint4*>(rows.p + row * rows.row + hk * rows.head + 8 * c) = out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int t = t0 + e;
+    if (t < first || t >= s.len) continue;
+    const uint4 v = held ? make_uint4(out[e][0], out[e][1], out[e][2], out[e][3]) : make_uint4(0u, 0u, 0u, 0u);
+    *reinterpret_cast<uint4*>(rows.p + (int64_t)(s.row0 + t - (s.len - s.n)) * rows.row + hk * rows.head + 8 * c) = v;
+  }
 }
 
 // ---- attention
@@ -385,12 +403,15 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
     }
   };
 
-  f32x4 acc[R][8];
-  float m[R], l[R];  // the offset, and the weights' total
+  // The weights' total is one more row of values, of ones: every lane of a row
+  // holds it, in all four of its elements.
+  f32x4 acc[R][8], total[R];
+  float m[R];  // the offset
+  const f16x8 ones = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
 #pragma unroll
   for (int t = 0; t < R; ++t) {
     m[t] = -INFINITY;
-    l[t] = 0.0f;
+    total[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int d = 0; d < 8; ++d) acc[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
@@ -467,7 +488,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
         const bool up = top[t] - m[t] > kSlack;
         const float alpha = up ? __builtin_amdgcn_exp2f(m[t] - top[t]) : 1.0f;
         m[t] = up ? top[t] : m[t];
-        l[t] *= alpha;
+        total[t] *= alpha;
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
       }
@@ -492,10 +513,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
         pw[t][h] = __builtin_bit_cast(
             f16x8, make_uint4(f16x2_bits(x[t][8 * h], x[t][8 * h + 1]), f16x2_bits(x[t][8 * h + 2], x[t][8 * h + 3]),
                               f16x2_bits(x[t][8 * h + 4], x[t][8 * h + 5]), f16x2_bits(x[t][8 * h + 6], x[t][8 * h + 7])));
-      float sum[4] = {x[t][0], x[t][1], x[t][2], x[t][3]};
 #pragma unroll
-      for (int e = 4; e < 16; ++e) sum[e & 3] += x[t][e];
-      l[t] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      for (int h = 0; h < 2; ++h) total[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[t][h], total[t], 0, 0, 0);
     }
 
     // ---- O^T += V^T P^T
@@ -520,8 +539,9 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
     page1 = page2;
     page2 = page3;
   }
+  float l[R];
 #pragma unroll
-  for (int t = 0; t < R; ++t) l[t] = fold_groups(l[t], [](float p, float r) { return p + r; }) * kTotalUnit;
+  for (int t = 0; t < R; ++t) l[t] = total[t][0] * kTotalUnit;
 
   // Where a row's result goes: its partial sums, or the output.
   auto write8 = [&](int row, int d, const float (&o)[8], float mx, float lsum) {
@@ -648,21 +668,21 @@ size_t workspace_of(const Attn4Plan& p, int T, int H) {
   return p.S > 1 ? kCounterRegionBytes + (size_t)p.S * T * H * (kD + 2) * sizeof(float) : 0;
 }
 
-// Groups of eight tokens that a batch's rows touch at most: (n + 14) / 8 of a
-// sequence with n rows, and no more than its rows.
-unsigned most_eights(const Cache4Batch& c) {
-  return (unsigned)std::min<int64_t>(c.T, ((int64_t)c.T + 14ll * std::min(c.B, c.T)) / kEight);
+// Groups of `size` tokens that a batch's rows touch at most: (n + 2 size - 2) /
+// size of a sequence with n rows, and no more than its rows.
+unsigned most_touched(const Cache4Batch& c, int size) {
+  return (unsigned)std::min<int64_t>(c.T, (c.T + (2ll * size - 2) * std::min(c.B, c.T)) / size);
 }
 
 }  // namespace
 
 hipError_t launch_cache4_append(const Cache4RowsArgs& a, hipStream_t stream) {
-  cache4_append<<<dim3(most_eights(a.c), (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
+  cache4_append<<<dim3(most_touched(a.c, kEight), (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_cache4_read(const Cache4RowsArgs& a, hipStream_t stream) {
-  cache4_read<<<dim3(most_eights(a.c), (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
+  cache4_read<<<dim3(most_touched(a.c, kBlock), (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
   return hipGetLastError();
 }
 
