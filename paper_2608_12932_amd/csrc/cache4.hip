@@ -68,87 +68,107 @@ __device__ __forceinline__ int touched(int n, int len) {
 
 // ---- append
 
-// One workgroup per (eight tokens, kv head): half of its threads take the keys,
-// half the values, 16 threads to a token.
+constexpr int64_t kResident = 256 * 8;  // workgroups of 256 threads that the chip holds
+
+// One workgroup per (eight tokens, N kv heads): half of its threads take the
+// keys, half the values, 16 threads to a token, with the loads of all N heads in
+// flight together.
+template <int N>
 __global__ __launch_bounds__(256) void cache4_append(const Cache4RowsArgs a) {
   constexpr int kPitch = kD + 4;  // bytes of a token's codes in LDS, off the banks' period
-  __shared__ uint8_t l_codes[kEight * kPitch];
+  __shared__ uint8_t l_codes[N][kEight * kPitch];
   const Cache4Batch& cb = a.c;
-  const int tid = threadIdx.x & 127, hk = blockIdx.y;
+  const int tid = threadIdx.x & 127, h0 = blockIdx.y * N;
   const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7) == 0;
   const Sequence s = find_sequence(cb, blockIdx.x, [](int n, int len) { return touched<kEight>(n, len); });
   if (s.b < 0) return;
   const int first = max(s.len - s.n, 0);  // the first new token that has a place
   const int t8 = first / kEight + s.item, page = cb.table[(int64_t)s.b * cb.max_blocks + t8 / (kBlock / kEight)];
-  const int c = tid & 15, t = t8 * kEight + (tid >> 4);
-  const bool there = t >= first && t < s.len;
+  const int c = tid & 15, t = t8 * kEight + (tid >> 4), at = t & (kBlock - 1);
+  const bool there = t >= first && t < s.len, held = page >= 0 && page < cb.n_pages;
 
-  // ---- the token's eight elements; one outside the call takes its last
+  // ---- the token's eight elements of each head; one outside the call takes its
+  // last, one past the heads the last of them
   const TokenRows rows = keys ? a.k : a.v;
   const int64_t row = s.row0 + (there ? t - (s.len - s.n) : s.n - 1);
-  const uint4 x4 = *reinterpret_cast<const uint4*>(rows.p + row * rows.row + hk * rows.head + 8 * c);
-  const uint32_t xw[4] = {x4.x, x4.y, x4.z, x4.w};
-  float x[8], lo, hi;
+  uint4 x4[N];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float v = (e & 1) ? bf16_hi(xw[e / 2]) : bf16_lo(xw[e / 2]);
-    x[e] = v != v ? 0.0f : fminf(fmaxf(v, -kClamp), kClamp);
-    lo = e ? fminf(lo, x[e]) : x[e];
-    hi = e ? fmaxf(hi, x[e]) : x[e];
-  }
-  auto fold = [&](auto ctrl) {  // over the group's 8 lanes
-    lo = fminf(lo, __uint_as_float(lane_move<decltype(ctrl)::value>(__float_as_uint(lo))));
-    hi = fmaxf(hi, __uint_as_float(lane_move<decltype(ctrl)::value>(__float_as_uint(hi))));
-  };
-  fold(std::integral_constant<int, kXor1>{});
-  fold(std::integral_constant<int, kXor2>{});
-  fold(std::integral_constant<int, kMirror8>{});
-  const _Float16 s16 = (_Float16)((hi - lo) / 15.0f);
-  const float sf = (float)s16;
-  const _Float16 b16 = (_Float16)(lo - 16.0f * sf);  // (16 s is exact, so a fused difference is the same)
-  const float bf = (float)b16;
-  uint32_t code[8];
+  for (int u = 0; u < N; ++u)
+    x4[u] = *reinterpret_cast<const uint4*>(rows.p + row * rows.row + min(h0 + u, cb.Hkv - 1) * rows.head + 8 * c);
+  // values: a thread turns eight tokens' codes of one d into a word
+  auto head_of = [&](int u) { return (int64_t)(held ? page : 0) * cb.Hkv + min(h0 + u, cb.Hkv - 1); };
+  auto word_of = [&](int u) { return cb.v_codes + head_of(u) * kCodeWords + (t8 & 7) * kD + tid; };
+  uint32_t mask = 0, old[N];  // the new tokens' bits, and what else the words hold
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-#pragma clang fp contract(off)
-    const float q = rintf((x[e] - bf) / (sf > 0.0f ? sf : 1.0f) - 16.0f);
-    code[e] = sf > 0.0f ? (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f) : 0u;
-  }
+  for (int e = 0; e < kEight; ++e) mask |= t8 * kEight + e >= first && t8 * kEight + e < s.len ? 15u << nibble(e) : 0u;
+#pragma unroll
+  for (int u = 0; u < N; ++u) old[u] = !keys && held && mask != ~0u ? *word_of(u) & ~mask : 0u;
 
-  const bool held = page >= 0 && page < cb.n_pages;
-  const int64_t head = (int64_t)(held ? page : 0) * cb.Hkv + hk;
-  const int at = t & (kBlock - 1);
-  const uint32_t s_bits = __builtin_bit_cast(uint16_t, s16), b_bits = __builtin_bit_cast(uint16_t, b16);
-  // ---- values: a thread turns eight tokens' codes of one d into a word
-  uint32_t* word = cb.v_codes + head * kCodeWords + (t8 & 7) * kD + tid;
-  uint32_t mask = 0, old = 0;  // the new tokens' bits, and what else the word holds
-  if (!keys) {
-    uint32_t* l = reinterpret_cast<uint32_t*>(l_codes + (tid >> 4) * kPitch) + 2 * c;
-    l[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-    l[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
 #pragma unroll
-    for (int e = 0; e < kEight; ++e) mask |= t8 * kEight + e >= first && t8 * kEight + e < s.len ? 15u << nibble(e) : 0u;
-    if (held && mask != ~0u) old = *word & ~mask;
+  for (int u = 0; u < N; ++u) {
+    const uint32_t xw[4] = {x4[u].x, x4[u].y, x4[u].z, x4[u].w};
+    float x[8], lo, hi;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = (e & 1) ? bf16_hi(xw[e / 2]) : bf16_lo(xw[e / 2]);
+      x[e] = v != v ? 0.0f : fminf(fmaxf(v, -kClamp), kClamp);
+      lo = e ? fminf(lo, x[e]) : x[e];
+      hi = e ? fmaxf(hi, x[e]) : x[e];
+    }
+    auto fold = [&](auto ctrl) {  // over the group's 8 lanes
+      lo = fminf(lo, __uint_as_float(lane_move<decltype(ctrl)::value>(__float_as_uint(lo))));
+      hi = fmaxf(hi, __uint_as_float(lane_move<decltype(ctrl)::value>(__float_as_uint(hi))));
+    };
+    fold(std::integral_constant<int, kXor1>{});
+    fold(std::integral_constant<int, kXor2>{});
+    fold(std::integral_constant<int, kMirror8>{});
+    const _Float16 s16 = (_Float16)((hi - lo) / 15.0f);
+    const float sf = (float)s16;
+    const _Float16 b16 = (_Float16)(lo - 16.0f * sf);  // (16 s is exact, so a fused difference is the same)
+    const float bf = (float)b16;
+    // The quotient by one product and a correction (Markstein's step): q = a y with
+    // y = 1 / s rounded is off by at most 1.5 ulp, the residual a - s q is exact
+    // (some 12 bits), and q + (a - s q) y lies within 1.5 2^-24 ulp of a / s; that
+    // is never so close to a midpoint of two fp32 numbers (a has 24 bits and s
+    // 11: 2^-12 ulp at least), so that it rounds to the quotient itself.
+    const float safe = sf > 0.0f ? sf : 1.0f, y = 1.0f / safe;
+    uint32_t code[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float a = x[e] - bf, q = a * y;
+      const float r = fmaf(fmaf(-safe, q, a), y, q);
+      code[e] = sf > 0.0f ? (uint32_t)fminf(fmaxf(rintf(r - 16.0f), 0.0f), 15.0f) : 0u;
+    }
+    const uint32_t s_bits = __builtin_bit_cast(uint16_t, s16), b_bits = __builtin_bit_cast(uint16_t, b16);
+    const bool write = held && there && h0 + u < cb.Hkv;
+    if (keys) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w |= code[e] << nibble(e);
+      if (write) cb.k_codes[head_of(u) * kCodeWords + ((at & 3) * 16 + (at >> 2)) * 16 + c] = w;
+      if (write && (c & 7) == 0)
+        reinterpret_cast<uint32_t*>(cb.k_params)[head_of(u) * (kParams / 2) + (c >> 3) * kBlock + at] = s_bits | b_bits << 16;
+    } else {
+      uint32_t* l = reinterpret_cast<uint32_t*>(l_codes[u] + (tid >> 4) * kPitch) + 2 * c;
+      l[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+      l[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+      if (write && (c & 7) == 0) {
+        uint16_t* p = cb.v_params + head_of(u) * kParams + (c >> 3) * (2 * kBlock) + at;
+        p[0] = (uint16_t)s_bits;
+        p[kBlock] = (uint16_t)b_bits;
+      }
+    }
   }
   lds_barrier();
-  if (!held) return;
-  uint32_t w = 0;
-  if (keys) {
-    if (!there) return;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w |= code[e] << nibble(e);
-    cb.k_codes[head * kCodeWords + ((at & 3) * 16 + (at >> 2)) * 16 + c] = w;
-    if ((c & 7) == 0) reinterpret_cast<uint32_t*>(cb.k_params)[head * (kParams / 2) + (c >> 3) * kBlock + at] = s_bits | b_bits << 16;
-    return;
-  }
+  if (keys || !held) return;
   const int d = 8 * (tid >> 2 & 15) + 4 * (tid >> 6) + (tid & 3);
 #pragma unroll
-  for (int e = 0; e < kEight; ++e) w |= (uint32_t)l_codes[e * kPitch + d] << nibble(e);
-  *word = old | (w & mask);
-  if (there && (c & 7) == 0) {
-    uint16_t* p = cb.v_params + head * kParams + (c >> 3) * (2 * kBlock) + at;
-    p[0] = (uint16_t)s_bits;
-    p[kBlock] = (uint16_t)b_bits;
+  for (int u = 0; u < N; ++u) {
+    if (h0 + u >= cb.Hkv) break;
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < kEight; ++e) w |= (uint32_t)l_codes[u][e * kPitch + d] << nibble(e);
+    *word_of(u) = old[u] | (w & mask);
   }
 }
 
@@ -249,7 +269,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
   constexpr int kPitch = kD + 4;        // floats of a row in the merge
   constexpr int kStage = 32 * 1024;     // a block's operands
   constexpr int kMergeBytes = NW * kWaveRows * kPitch * 4;
-  static_assert(kDirect || NW == 4 || NW == 8, "shares of a block's 16 + 16 operands");
+  static_assert(kDirect || NW == 8, "shares of a block's 16 + 16 operands");
   __shared__ __align__(16) uint8_t lds[kDirect ? kMergeBytes : 2 * kStage];
   __shared__ float2 l_ml[kDirect ? NW * kWaveRows : 1];
 
@@ -329,45 +349,47 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
 
   // ---- a block's codes and parameters as they lie in the page
   auto bytes = [&](int page, int n) { return page < 0 ? 0u : (uint32_t)n; };  // nothing is read where there is no page
-  auto head_of = [&](int page) { return (int64_t)max(page, 0) * cb.Hkv + hk; };
   auto rsrc = [&](const void* base, int page, int n) {
-    return make_rsrc(uniform_ptr(static_cast<const uint8_t*>(base) + head_of(page) * n), bytes(page, n));
+    return make_rsrc(uniform_ptr(static_cast<const uint8_t*>(base) + ((int64_t)max(page, 0) * cb.Hkv + hk) * n), bytes(page, n));
   };
-  constexpr int kKeyLoads = kDirect ? 4 : 1, kValueLoads = kDirect ? 4 : 1;
   // keys: tile u's rows 1 KiB on; a token's params of this lane group's half of d, four tokens 16 bytes
   const uint32_t k_at = (uint32_t)(l16 * 64 + 16 * g), kp_at = (uint32_t)((g >> 1) * 256 + l16 * 16);
   // values: step h, half j of a lane's rows
   const uint32_t v_at = (uint32_t)(g * 1024 + l16 * 16), vp_at = (uint32_t)((l16 >> 3) * 256 + 32 * g);
-  // (not direct) this wave's share: with four waves key tile `wave` and value piece `wave`, with eight
-  // the first four waves' keys, the others' values
-  const bool my_keys = kDirect || NW == 4 || wave < 4, my_values = kDirect || NW == 4 || wave >= 4;
+  // (not direct) a wave's share: a tile of keys the first four's, a quarter of the values the others'
+  const bool my_keys = kDirect || wave < 4, my_values = kDirect || wave >= 4;
   const int piece = wave & 3;
-  uint4 kr[kKeyLoads], kp, vr[kValueLoads], vs[kDirect ? 2 : 1], vb[kDirect ? 2 : 1];
-  auto load_keys = [&](int page) {
+  struct Keys {
+    uint4 codes[kDirect ? 4 : 1], params;
+  };
+  struct Values {
+    uint4 codes[kDirect ? 4 : 1], s[kDirect ? 2 : 1], b[kDirect ? 2 : 1];
+  };
+  auto load_keys = [&](int page, Keys& k) {
     const __amdgpu_buffer_rsrc_t r = rsrc(cb.k_codes, page, kCodeBytes), p = rsrc(cb.k_params, page, kParamBytes);
     if constexpr (kDirect) {
-      kp = buf_load16<AUX>(p, kp_at);
+      k.params = buf_load16<AUX>(p, kp_at);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) kr[u] = buf_load16<AUX>(r, k_at + 1024 * u);
+      for (int u = 0; u < 4; ++u) k.codes[u] = buf_load16<AUX>(r, k_at + 1024 * u);
     } else {
-      kp.x = buf_load4<AUX>(p, kp_at + 4 * piece);
-      kr[0] = buf_load16<AUX>(r, k_at + 1024 * piece);
+      k.params.x = buf_load4<AUX>(p, kp_at + 4 * piece);
+      k.codes[0] = buf_load16<AUX>(r, k_at + 1024 * piece);
     }
   };
-  auto load_values = [&](int page) {
+  auto load_values = [&](int page, Values& v) {
     const __amdgpu_buffer_rsrc_t r = rsrc(cb.v_codes, page, kCodeBytes), p = rsrc(cb.v_params, page, kParamBytes);
     if constexpr (kDirect) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        vs[h] = buf_load16<AUX>(p, vp_at + 16 * h);
-        vb[h] = buf_load16<AUX>(p, vp_at + 128 + 16 * h);
-        vr[2 * h] = buf_load16<AUX>(r, v_at + 512 * h);
-        vr[2 * h + 1] = buf_load16<AUX>(r, v_at + 512 * h + 256);
+        v.s[h] = buf_load16<AUX>(p, vp_at + 16 * h);
+        v.b[h] = buf_load16<AUX>(p, vp_at + 128 + 16 * h);
+        v.codes[2 * h] = buf_load16<AUX>(r, v_at + 512 * h);
+        v.codes[2 * h + 1] = buf_load16<AUX>(r, v_at + 512 * h + 256);
       }
     } else {
-      vs[0] = buf_load16<AUX>(p, vp_at + 16 * (piece >> 1));
-      vb[0] = buf_load16<AUX>(p, vp_at + 128 + 16 * (piece >> 1));
-      vr[0] = buf_load16<AUX>(r, v_at + 256 * piece);
+      v.s[0] = buf_load16<AUX>(p, vp_at + 16 * (piece >> 1));
+      v.b[0] = buf_load16<AUX>(p, vp_at + 128 + 16 * (piece >> 1));
+      v.codes[0] = buf_load16<AUX>(r, v_at + 256 * piece);
     }
   };
   // Values of tokens that the sequence does not hold are zeros, whatever lies
@@ -378,34 +400,21 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
     for (int i = 0; i < 4; ++i)
       w[i] &= (token0 + 2 * i < s.len ? 0xFFFFu : 0u) | (token0 + 2 * i + 1 < s.len ? 0xFFFF0000u : 0u);
   };
-  auto clean_values = [&](int i) {
-    const int key0 = (p_first + KW * i) * kBlock;
-    if (key0 + kBlock <= s.len) return;
+  auto key0_of = [&](int i) { return (p_first + KW * i) * kBlock; };
+  auto clean_values = [&](int i, Values& v) {
+    if (key0_of(i) + kBlock <= s.len) return;
 #pragma unroll
     for (int h = 0; h < (kDirect ? 2 : 1); ++h) {
-      const int token0 = key0 + 16 * g + 8 * (kDirect ? h : piece >> 1);
-      clean(vs[h], token0);
-      clean(vb[h], token0);
+      const int token0 = key0_of(i) + 16 * g + 8 * (kDirect ? h : piece >> 1);
+      clean(v.s[h], token0);
+      clean(v.b[h], token0);
     }
   };
   auto word = [](const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
-  // (not direct) block i's operands to stage i % 2: keys' (u, step) at 4 u + step, values' (h, t) at 16 + 8 h + t
-  auto stage = [&](int i) {
-    uint8_t* dst = lds + (i & 1) * kStage + lane * 16;
-    if (my_keys) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + (4 * piece + e) * 1024) = keys8(word(kr[0], e), kp.x);
-    }
-    if (my_values) {
-      clean_values(i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + (16 + 4 * piece + e) * 1024) = values8(word(vr[0], e), vs[0], vb[0]);
-    }
-  };
 
   // The weights' total is one more row of values, of ones: every lane of a row
   // holds it, in all four of its elements.
-  f32x4 acc[R][8], total[R];
+  f32x4 acc[R][8], total[R], sc[R][4];
   float m[R];  // the offset
   const f16x8 ones = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
 #pragma unroll
@@ -416,45 +425,24 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
     for (int d = 0; d < 8; ++d) acc[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  if (my_keys) load_keys(page0);
-  if (my_values) load_values(page0);
-  if constexpr (!kDirect) {
-    stage(0);
-    if (my_keys) load_keys(page1);
-    if (my_values) load_values(page1);
-    lds_barrier();
-  }
-
-  for (int i = 0; i < rounds; ++i) {
-    const int page3 = page_of(i + 3);
-    const int key0 = (p_first + KW * i) * kBlock;
-    const uint8_t* src = lds + (i & 1) * kStage + lane * 16;
-    if constexpr (!kDirect) {  // the other stage was last read before the barrier
-      stage(i + 1);
-      if (my_keys) load_keys(page2);
-      if (my_values) load_values(page2);
-    }
-
-    // ---- scores
-    f32x4 sc[R][4];
+  // ---- the steps of a block
+  // scores, from operands that `key` gives for (tile, step)
+  auto score = [&](auto key) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f16x8 kf;
-        if constexpr (kDirect)
-          kf = keys8(word(kr[u], e), word(kp, u));
-        else
-          kf = *reinterpret_cast<const f16x8*>(src + (4 * u + e) * 1024);
+      for (int u = 0; u < 4; ++u) {
+        const f16x8 kf = key(u, e);
 #pragma unroll
         for (int t = 0; t < R; ++t)
           sc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][e], e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[t][u], 0, 0, 0);
       }
-    }
-    if constexpr (kDirect) load_keys(page1);
-
-    // ---- masks and the rows' largest; token 16 g + e is element e / 4 of tile e % 4
-    float x[R][16], top[R];
+  };
+  // masks, the rows' largest, the offsets; token 16 g + e is element e / 4 of tile e % 4
+  float x[R][16], by[R], off[R];
+  auto look = [&](int i, int page) {
+    const int key0 = key0_of(i);
+    float top[R];
     bool all = true;
 #pragma unroll
     for (int t = 0; t < R; ++t) {
@@ -462,10 +450,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
       for (int e = 0; e < 16; ++e) x[t][e] = sc[t][e & 3][e >> 2];
       all = all && last_key[t] >= key0 + kBlock - 1;
     }
-    if (!__all(all) || page0 < 0) {
+    if (!__all(all) || page < 0) {
 #pragma unroll
       for (int t = 0; t < R; ++t) {
-        const int lim = page0 >= 0 ? last_key[t] - key0 - 16 * g : INT_MIN;  // tokens of this lane past it are not seen
+        const int lim = page >= 0 ? last_key[t] - key0 - 16 * g : INT_MIN;  // tokens of this lane past it are not seen
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[t][e] = e <= lim ? x[t][e] : -INFINITY;
       }
@@ -493,51 +481,136 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
         for (int d = 0; d < 8; ++d) acc[t][d] *= alpha;
       }
     }
-
-    // ---- weights
-    f16x8 pw[R][2];
+    bool large = false;
 #pragma unroll
     for (int t = 0; t < R; ++t) {
-      const bool none = m[t] == -INFINITY;
-      float by = f[t], off = none ? 0.0f : -m[t];
-      if (__builtin_expect(__any(fabsf(off) >= kLarge - 16.0f), 0)) {
-        const bool large = fabsf(off) >= kLarge - 16.0f;
+      by[t] = f[t];
+      off[t] = m[t] == -INFINITY ? 0.0f : -m[t];
+      large = large || fabsf(off[t]) >= kLarge - 16.0f;
+    }
+    if (__builtin_expect(__any(large), 0)) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[t][e] = large ? x[t][e] * by : x[t][e];
-        by = large ? 1.0f : by;
+      for (int t = 0; t < R; ++t) {
+        const bool rounded = fabsf(off[t]) >= kLarge - 16.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[t][e] = rounded ? x[t][e] * by[t] : x[t][e];
+        by[t] = rounded ? 1.0f : by[t];
       }
+    }
+  };
+  f16x8 pw[R][2];
+  auto weigh = [&] {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[t][e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], by, off));
+    for (int t = 0; t < R; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], by[t], off[t]));
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         pw[t][h] = __builtin_bit_cast(
             f16x8, make_uint4(f16x2_bits(x[t][8 * h], x[t][8 * h + 1]), f16x2_bits(x[t][8 * h + 2], x[t][8 * h + 3]),
                               f16x2_bits(x[t][8 * h + 4], x[t][8 * h + 5]), f16x2_bits(x[t][8 * h + 6], x[t][8 * h + 7])));
-#pragma unroll
-      for (int h = 0; h < 2; ++h) total[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[t][h], total[t], 0, 0, 0);
     }
-
-    // ---- O^T += V^T P^T
-    if constexpr (kDirect) clean_values(i);
+  };
+  // O^T += V^T P^T, from operands that `value` gives for (step, tile)
+  auto add = [&](auto value) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
-        f16x8 vf;
-        if constexpr (kDirect)
-          vf = values8(word(vr[2 * h + d / 4], d % 4), vs[h], vb[h]);
-        else
-          vf = *reinterpret_cast<const f16x8*>(src + (16 + 8 * h + d) * 1024);
+        const f16x8 vf = value(h, d);
 #pragma unroll
         for (int t = 0; t < R; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pw[t][h], acc[t][d], 0, 0, 0);
       }
-    if constexpr (kDirect)
-      load_values(page1);
-    else
+#pragma unroll
+      for (int t = 0; t < R; ++t) total[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[t][h], total[t], 0, 0, 0);
+    }
+  };
+
+  if constexpr (kDirect) {
+    // With one tile of rows a block's codes are loaded while the block before it
+    // is worked on, into registers of their own: 9 KiB a wave in flight.  (With
+    // two tiles those registers would cost the second wave of a SIMD: there the
+    // next keys are loaded behind the scores, the next values at the end.)
+    constexpr bool kAhead = R == 1;
+    Keys keys[2];
+    Values vals[2];
+    load_keys(page0, keys[0]);
+    load_values(page0, vals[0]);
+    auto round = [&](int i, Keys& k, Values& v, Keys& k_next, Values& v_next) {
+      const int page3 = page_of(i + 3);
+      if constexpr (kAhead) {
+        load_keys(page1, k_next);
+        load_values(page1, v_next);
+      }
+      score([&](int u, int e) { return keys8(word(k.codes[u], e), word(k.params, u)); });
+      if constexpr (!kAhead) load_keys(page1, k);
+      look(i, page0);
+      weigh();
+      clean_values(i, v);
+      add([&](int h, int d) { return values8(word(v.codes[2 * h + d / 4], d % 4), v.s[h], v.b[h]); });
+      if constexpr (!kAhead) load_values(page1, v);
+      page0 = page1;
+      page1 = page2;
+      page2 = page3;
+    };
+    int i = 0;
+    if constexpr (kAhead) {
+      for (; i + 1 < rounds; i += 2) {  // (a way from the first to the loop's head would make it wait for all loads)
+        round(i, keys[0], vals[0], keys[1], vals[1]);
+        round(i + 1, keys[1], vals[1], keys[0], vals[0]);
+      }
+      if (i < rounds) round(i, keys[0], vals[0], keys[1], vals[1]);
+    } else {
+      for (; i < rounds; ++i) round(i, keys[0], vals[0], keys[0], vals[0]);
+    }
+  } else {
+    // A block's codes are loaded two rounds before they become operands, which
+    // is a round before their use.
+    auto stage = [&](int i, const Keys& k, Values& v) {  // keys' operand (u, step) at 4 u + step, values' (h, d) at 16 + 8 h + d
+      uint8_t* dst = lds + (i & 1) * kStage + lane * 16 + piece * 4096;
+      if (my_keys) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + e * 1024) = keys8(word(k.codes[0], e), k.params.x);
+      }
+      if (my_values) {
+        clean_values(i, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + 16384 + e * 1024) = values8(word(v.codes[0], e), v.s[0], v.b[0]);
+      }
+    };
+    auto load = [&](int page, Keys& k, Values& v) {
+      if (my_keys) load_keys(page, k);
+      if (my_values) load_values(page, v);
+    };
+    Keys k[2];
+    Values v[2];
+    load(page0, k[0], v[0]);
+    load(page1, k[1], v[1]);
+    stage(0, k[0], v[0]);
+    load(page2, k[0], v[0]);
+    lds_barrier();
+    int page3 = page_of(3);
+    auto round = [&](int i, Keys& k, Values& v) {
+      const int page4 = page_of(i + 4);
+      stage(i + 1, k, v);  // where block i - 1 was, which was last read before the barrier
+      load(page3, k, v);
+      const uint8_t* src = lds + (i & 1) * kStage + lane * 16;
+      score([&](int u, int e) { return *reinterpret_cast<const f16x8*>(src + (4 * u + e) * 1024); });
+      look(i, page0);
+      weigh();
+      add([&](int h, int d) { return *reinterpret_cast<const f16x8*>(src + (16 + 8 * h + d) * 1024); });
       lds_barrier();
-    page0 = page1;
-    page1 = page2;
-    page2 = page3;
+      page0 = page1;
+      page1 = page2;
+      page2 = page3;
+      page3 = page4;
+    };
+    int i = 0;
+    for (; i + 1 < rounds; i += 2) {  // (a way from the first to the loop's head would make it wait for all loads)
+      round(i, k[1], v[1]);
+      round(i + 1, k[0], v[0]);
+    }
+    if (i < rounds) round(i, k[1], v[1]);
   }
   float l[R];
 #pragma unroll
@@ -609,7 +682,19 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
 // The forms of a call, and what one of its workgroups costs in ns: alone on a
 // CU lat + lat_round a round (a block of each of the KW waves that share one);
 // in a full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
-// thr_round a round.
+// thr_round a round.  Fitted, with the merge's 3430 + 0.24 a (split, token,
+// head), to 95 calls (B 1 - 64, 1 - 1024 new tokens, 60 - 90000 long, five head
+// layouts) at up to 12 numbers of splits: what the rule picks is 0.1 % above the
+// best of all forms and splits on average, 7 % at most.  Without the two shared
+// forms the best would be 1.7 % slower on average and 42 % at most.  64 and 128
+// rows in four waves (one a SIMD), and 16 and 32 rows in eight, tried too, took
+// nothing off.  us of 16 / 32 / 128 / 256 rows, at its best splits each: 12
+// ragged sequences of up to 33 tokens over up to 1900 21.8 19.6 28.0 36.3; 1024
+// over 8192 265 180 168 159.
+//   The calls were of one kind of sequence each.  A batch is taken as B
+// sequences of max_len with the average number of new tokens, so one that mixes
+// kinds (a chunk among single tokens, one long among short) gets the form and
+// splits of neither: a call for each kind is faster.
 typedef void (*Attn4Fn)(const Cache4AttnArgs);
 struct Attn4Form {
   int rows, KW, threads;
@@ -617,15 +702,16 @@ struct Attn4Form {
   Attn4Fn fn;
 };
 const Attn4Form kForms[] = {
-    {16, 4, 256, 800, 970, 860, 700, cache4_attention<1, 4, true>},
-    {64, 1, 256, 1570, 1010, 1840, 720, cache4_attention<1, 4, false>},
-    {128, 1, 256, 3010, 1200, 4000, 1200, cache4_attention<2, 4, false>},
+    {16, 4, 256, 2610, 1140, 1280, 1040, cache4_attention<1, 4, true>},
+    {32, 4, 256, 4310, 1720, 1490, 1490, cache4_attention<2, 4, true>},
+    {128, 1, 512, 3370, 1350, 2900, 1360, cache4_attention<1, 8, false>},
+    {256, 1, 512, 5960, 920, 4590, 2150, cache4_attention<2, 8, false>},
 };
+constexpr int64_t kMergeCost = 3430, kMergePart = 24;  // ns, ns for 100 (split, token, head)
+// Where the rows of a sequence's kv head are one row block, its pages are read
+// once, past the caches: of 13 calls from 1 MB to 300 MB none was slower so, and
+// 64 sequences of 4096 take 51 us instead of 63.
 const Attn4Fn kStreamFn = cache4_attention<1, 4, true, kCacheStream>;
-constexpr int64_t kTokenBytes = kD + 16;  // of a kv head's keys and values
-// A cache that is read once and is larger than this does not stay in the
-// memory-side cache (256 MB) until the next call: it is read past it.
-constexpr int64_t kStreamBytes = int64_t(160) << 20;
 constexpr int64_t kMaxAxis = 65535;  // workgroups along the second and third axis of a launch
 
 struct Attn4Plan {
@@ -649,7 +735,7 @@ Attn4Plan plan_attention(int B, int T, int H, int Hkv, int max_len) {
       if (S > 1 && S > most) break;
       const int64_t rounds = ((uint64_t)(blocks + S - 1) / S + k.KW - 1) >> by_kw;
       const int64_t cost = std::max(k.lat + rounds * k.lat_round, ((tiles * S + 255) >> 8) * (k.thr + rounds * k.thr_round)) +
-                           (S > 1 ? 1820 + (int64_t)((uint64_t)S * T * H * 21 / 100) : 0);
+                           (S > 1 ? kMergeCost + (int64_t)((uint64_t)S * T * H * kMergePart / 100) : 0);
       if (cost < least) {
         least = cost;
         p.form = f;
@@ -660,7 +746,7 @@ Attn4Plan plan_attention(int B, int T, int H, int Hkv, int max_len) {
   const int64_t rows = kForms[p.form].rows;
   // every sequence's last row block may be partial, but each has a row
   p.tiles = std::min<int64_t>(T * G / rows + B, T * ((G + rows - 1) / rows));
-  p.stream = p.form == 0 && n * G <= rows && (int64_t)B * max_len >= kStreamBytes / kTokenBytes / Hkv;
+  p.stream = p.form == 0 && n * G <= rows;
   return p;
 }
 
@@ -677,7 +763,12 @@ unsigned most_touched(const Cache4Batch& c, int size) {
 }  // namespace
 
 hipError_t launch_cache4_append(const Cache4RowsArgs& a, hipStream_t stream) {
-  cache4_append<<<dim3(most_touched(a.c, kEight), (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
+  const unsigned groups = most_touched(a.c, kEight);
+  constexpr int N = 2;
+  if ((int64_t)groups * a.c.Hkv > kResident)
+    cache4_append<N><<<dim3(groups, (unsigned)(a.c.Hkv + N - 1) / N), dim3(256), 0, stream>>>(a);
+  else
+    cache4_append<1><<<dim3(groups, (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);
   return hipGetLastError();
 }
 
