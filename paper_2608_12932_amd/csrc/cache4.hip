@@ -256,27 +256,34 @@ constexpr float kLarge = 0x1p23f;
 //   - row m of value tile t is d = 8 m + t, so that a lane's rows share a group
 //     and its eight outputs are 16 bytes of a row.
 //
-// Direct: the waves share the rows and take every NW-th block each, reading
-// operands straight from the page (a load instruction covers 1 KiB of keys),
-// and meet in LDS at the end.  Otherwise the waves hold different rows of the
-// same blocks, turn a share of each block into fp16 operands and hand them round
-// through LDS, a block ahead of their use; operand order, 1 KiB an operand, so
-// no access meets a bank twice.
-template <int R, int NW, bool kDirect, int AUX = kCacheDefault>
+// Of NW waves KW groups hold the same rows and take every KW-th block each,
+// meeting in LDS at the end; the waves of a group hold different rows of the same
+// blocks.  A group of one wave reads its operands straight from the page (a load
+// instruction covers 1 KiB of keys).  A larger one turns a share of each block a
+// wave into fp16 operands and hands them round through LDS, a block ahead of
+// their use; operand order, 1 KiB an operand, so no access meets a bank twice.
+//
+// 64 single tokens over 4096: 51 us, 6.0 TB/s of cache, bound by HBM and, behind
+// it, by the vector unit (384 of some 500 instructions a block turn codes into
+// fp16).  1024 tokens over 8192: 160 us, 0.86 PFLOP/s, bound by vector and matrix
+// instructions, which share a SIMD's issue: a wave's vector instructions beside
+// another's MFMAs take half of the MFMAs' time on top of their own (8 MFMAs 172
+// cycles, 32 multiply-adds 188, both together 272).
+template <int R, int KW, int NW, int AUX = kCacheDefault>
 __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnArgs a) {
-  constexpr int kWaveRows = 16 * R, kRows = kDirect ? kWaveRows : NW * kWaveRows;
-  constexpr int KW = kDirect ? NW : 1;  // waves that share the blocks of the same rows
-  constexpr int kPitch = kD + 4;        // floats of a row in the merge
-  constexpr int kStage = 32 * 1024;     // a block's operands
-  constexpr int kMergeBytes = NW * kWaveRows * kPitch * 4;
-  static_assert(kDirect || NW == 8, "shares of a block's 16 + 16 operands");
-  __shared__ __align__(16) uint8_t lds[kDirect ? kMergeBytes : 2 * kStage];
-  __shared__ float2 l_ml[kDirect ? NW * kWaveRows : 1];
+  constexpr int kWaveRows = 16 * R, kSame = NW / KW, kRows = kSame * kWaveRows;
+  constexpr bool kDirect = kSame == 1;
+  constexpr int kPitch = kD + 4;     // floats of a row in the merge
+  constexpr int kStage = 32 * 1024;  // a block's operands
+  constexpr int kMergeBytes = KW > 1 ? NW * kWaveRows * kPitch * 4 : 0;
+  static_assert(kDirect || kSame == 4 || kSame == 8, "shares of a block's 16 + 16 operands");
+  __shared__ __align__(16) uint8_t lds[std::max(kDirect ? 0 : KW * 2 * kStage, kMergeBytes)];
+  __shared__ float2 l_ml[KW > 1 ? NW * kWaveRows : 1];
 
   const Cache4Batch& cb = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int G = a.G, kw = kDirect ? wave : 0, same = kDirect ? 0 : wave;
+  const int G = a.G, kw = wave / kSame, same = wave % kSame;
   // Workgroups of neighbouring kv heads go to the XCDs in turn, so that all of
   // a head's row blocks find its pages in one L2.
   const int hk = blockIdx.x;
@@ -299,7 +306,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
   const int seen = s.len - s.n + token_of(min(wg_row0 + kRows, n_rows) - 1 - wg_row0) + 1;
   const int blocks = (max(seen, 0) + kBlock - 1) / kBlock, per = a.by_s.divide(blocks + a.S - 1);
   const int p_begin = split * per, p_end = min(p_begin + per, blocks);
-  const int p_first = p_begin + kw, rounds = max(p_end - p_first + KW - 1, 0) / KW;  // blocks p_first + KW i < p_end
+  // the wave's blocks p_first + KW i < p_end; waves that meet at barriers make the same number of rounds
+  const int p_first = p_begin + kw, rounds = max(p_end - (kDirect ? p_first : p_begin) + KW - 1, 0) / KW;
 
   // The page of block i, -1: none (past the split's, or out of the pool: tokens that no row sees)
   typedef const __attribute__((address_space(4))) int32_t* ConstTable;
@@ -356,9 +364,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
   const uint32_t k_at = (uint32_t)(l16 * 64 + 16 * g), kp_at = (uint32_t)((g >> 1) * 256 + l16 * 16);
   // values: step h, half j of a lane's rows
   const uint32_t v_at = (uint32_t)(g * 1024 + l16 * 16), vp_at = (uint32_t)((l16 >> 3) * 256 + 32 * g);
-  // (not direct) a wave's share: a tile of keys the first four's, a quarter of the values the others'
-  const bool my_keys = kDirect || wave < 4, my_values = kDirect || wave >= 4;
-  const int piece = wave & 3;
+  // (not direct) a wave's share of its group's blocks: of four waves each a tile of keys and a quarter of
+  // the values, of eight the first four the keys, the others the values
+  const bool my_keys = kSame < 8 || same < 4, my_values = kSame < 8 || same >= 4;
+  const int piece = same & 3;
   struct Keys {
     uint4 codes[kDirect ? 4 : 1], params;
   };
@@ -564,10 +573,11 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
       for (; i < rounds; ++i) round(i, keys[0], vals[0], keys[0], vals[0]);
     }
   } else {
+    uint8_t* l_group = lds + kw * 2 * kStage;
     // A block's codes are loaded two rounds before they become operands, which
     // is a round before their use.
     auto stage = [&](int i, const Keys& k, Values& v) {  // keys' operand (u, step) at 4 u + step, values' (h, d) at 16 + 8 h + d
-      uint8_t* dst = lds + (i & 1) * kStage + lane * 16 + piece * 4096;
+      uint8_t* dst = l_group + (i & 1) * kStage + lane * 16 + piece * 4096;
       if (my_keys) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + e * 1024) = keys8(word(k.codes[0], e), k.params.x);
@@ -594,7 +604,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
       const int page4 = page_of(i + 4);
       stage(i + 1, k, v);  // where block i - 1 was, which was last read before the barrier
       load(page3, k, v);
-      const uint8_t* src = lds + (i & 1) * kStage + lane * 16;
+      const uint8_t* src = l_group + (i & 1) * kStage + lane * 16;
       score([&](int u, int e) { return *reinterpret_cast<const f16x8*>(src + (4 * u + e) * 1024); });
       look(i, page0);
       weigh();
@@ -630,8 +640,9 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
       *reinterpret_cast<uint4*>(a.o.p + tok * a.o.row + h * a.o.head + d) = output8(o, lsum);
     }
   };
-  if constexpr (kDirect) {
-    // the waves' partial results of the same rows meet in LDS
+  if constexpr (KW > 1) {
+    // the partial results of the waves with the same rows meet in LDS
+    if constexpr (!kDirect) lds_barrier();  // (where the stages were)
     float* l_o = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int t = 0; t < R; ++t) {
@@ -650,10 +661,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
       if (row >= n_rows) continue;
       float mx = -INFINITY, lsum = 0.0f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < NW; ++w) mx = fmaxf(mx, l_ml[r + w * kRows].x);
+      for (int w = 0; w < KW; ++w) mx = fmaxf(mx, l_ml[r + w * kRows].x);
       const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
+      for (int w = 0; w < KW; ++w) {
         const float2 ml = l_ml[r + w * kRows];
         const float by = __builtin_amdgcn_exp2f(ml.x - base);
         lsum = fmaf(ml.y, by, lsum);
@@ -680,17 +691,17 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
 }
 
 // The forms of a call, and what one of its workgroups costs in ns: alone on a
-// CU lat + lat_round a round (a block of each of the KW waves that share one);
-// in a full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
+// CU lat + lat_round a round (a block of each of the KW groups of waves); in a
+// full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
 // thr_round a round.  Fitted, with the merge's 3430 + 0.24 a (split, token,
 // head), to 95 calls (B 1 - 64, 1 - 1024 new tokens, 60 - 90000 long, five head
 // layouts) at up to 12 numbers of splits: what the rule picks is 0.1 % above the
-// best of all forms and splits on average, 7 % at most.  Without the two shared
-// forms the best would be 1.7 % slower on average and 42 % at most.  64 and 128
-// rows in four waves (one a SIMD), and 16 and 32 rows in eight, tried too, took
-// nothing off.  us of 16 / 32 / 128 / 256 rows, at its best splits each: 12
-// ragged sequences of up to 33 tokens over up to 1900 21.8 19.6 28.0 36.3; 1024
-// over 8192 265 180 168 159.
+// best of all forms and splits on average, 2 % at most.  Without the three
+// shared forms the best would be 1.7 % slower on average and 42 % at most,
+// without the last 0.1 % and 8 %.  64 and 128 rows in four waves (one a SIMD),
+// and 16 and 32 rows in eight, tried too, took nothing off.  us of the five, at
+// its best splits each: 12 ragged sequences of up to 33 tokens over up to 1900 21
+// 19 28 36 29; 256 over 4096 - 35 41 46 38; 1024 over 8192 265 192 179 167 160.
 //   The calls were of one kind of sequence each.  A batch is taken as B
 // sequences of max_len with the average number of new tokens, so one that mixes
 // kinds (a chunk among single tokens, one long among short) gets the form and
@@ -702,16 +713,17 @@ struct Attn4Form {
   Attn4Fn fn;
 };
 const Attn4Form kForms[] = {
-    {16, 4, 256, 2610, 1140, 1280, 1040, cache4_attention<1, 4, true>},
-    {32, 4, 256, 4310, 1720, 1490, 1490, cache4_attention<2, 4, true>},
-    {128, 1, 512, 3370, 1350, 2900, 1360, cache4_attention<1, 8, false>},
-    {256, 1, 512, 5960, 920, 4590, 2150, cache4_attention<2, 8, false>},
+    {16, 4, 256, 2420, 1140, 1200, 1030, cache4_attention<1, 4, 4>},
+    {32, 4, 256, 3240, 1650, 1550, 1470, cache4_attention<2, 4, 4>},
+    {128, 1, 512, 3310, 1370, 2820, 1370, cache4_attention<1, 1, 8>},
+    {256, 1, 512, 3510, 1690, 4700, 2120, cache4_attention<2, 1, 8>},
+    {128, 2, 512, 7240, 830, 5420, 2310, cache4_attention<2, 2, 8>},
 };
 constexpr int64_t kMergeCost = 3430, kMergePart = 24;  // ns, ns for 100 (split, token, head)
 // Where the rows of a sequence's kv head are one row block, its pages are read
 // once, past the caches: of 13 calls from 1 MB to 300 MB none was slower so, and
 // 64 sequences of 4096 take 51 us instead of 63.
-const Attn4Fn kStreamFn = cache4_attention<1, 4, true, kCacheStream>;
+const Attn4Fn kStreamFn = cache4_attention<1, 4, 4, kCacheStream>;
 constexpr int64_t kMaxAxis = 65535;  // workgroups along the second and third axis of a launch
 
 struct Attn4Plan {
