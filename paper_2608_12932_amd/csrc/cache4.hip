@@ -72,7 +72,10 @@ constexpr int64_t kResident = 256 * 8;  // workgroups of 256 threads that the ch
 
 // One workgroup per (eight tokens, N kv heads): half of its threads take the
 // keys, half the values, 16 threads to a token, with the loads of all N heads in
-// flight together.
+// flight together.  Bound by a chain of reads (batch, page, words) and, with many
+// tokens, by the vector unit beside it: 16 single tokens of 8 heads 3.5 us, 3288
+// tokens 8.9 (17 MB; 9.6 with one head a workgroup, 10.3 with four; 11.3 with
+// whole divisions).
 template <int N>
 __global__ __launch_bounds__(256) void cache4_append(const Cache4RowsArgs a) {
   constexpr int kPitch = kD + 4;  // bytes of a token's codes in LDS, off the banks' period
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(256) void cache4_read(const Cache4RowsArgs a) {
     const int t = t0 + e;
     if (t < first || t >= s.len) continue;
     const uint4 v = held ? make_uint4(out[e][0], out[e][1], out[e][2], out[e][3]) : make_uint4(0u, 0u, 0u, 0u);
-    *reinterpret_cast<uint4*>(rows.p + (int64_t)(s.row0 + t - (s.len - s.n)) * rows.row + hk * rows.head + 8 * c) = v;
+    stg_nt(reinterpret_cast<uint4*>(rows.p + (int64_t)(s.row0 + t - (s.len - s.n)) * rows.row + hk * rows.head + 8 * c), v);
   }
 }
 
@@ -777,7 +780,7 @@ unsigned most_touched(const Cache4Batch& c, int size) {
 hipError_t launch_cache4_append(const Cache4RowsArgs& a, hipStream_t stream) {
   const unsigned groups = most_touched(a.c, kEight);
   constexpr int N = 2;
-  if ((int64_t)groups * a.c.Hkv > kResident)
+  if ((int64_t)groups * a.c.Hkv > kResident)  // more than one round of workgroups
     cache4_append<N><<<dim3(groups, (unsigned)(a.c.Hkv + N - 1) / N), dim3(256), 0, stream>>>(a);
   else
     cache4_append<1><<<dim3(groups, (unsigned)a.c.Hkv), dim3(256), 0, stream>>>(a);

@@ -203,6 +203,16 @@ def test_tokens_taken_back(L, back):
     m.check_attention([1, 1], 4)
 
 
+def test_more_new_tokens_than_the_sequence_holds():
+    # the last of them are held
+    m = Model(2, 2, 64, seed=40)
+    k, v = m.values(30, 2), m.values(30, 2)
+    kd, vd = bf16_dev(k), bf16_dev(v)
+    w.w4a8_cache4_append(kd, vd, m.cache, i32([0, 20, 30]), i32([13, 10]), i32(m.table))
+    m.k, m.v = [k[7:20], k[20:]], [v[7:20], v[20:]]
+    m.check_pages()
+
+
 def test_special_values():
     m = Model(1, 1, 64, seed=4)
     k, v = m.values(16, 1), m.values(16, 1)
@@ -781,3 +791,35 @@ def test_a_layer_step_by_step(axes):
         ref = oracle.linear(to_np_bits(o).reshape(n, H * D), Wo, s_w=so)
         np.testing.assert_array_equal(to_np_bits(y), ref["y"])
     m.check_pages()
+
+
+# Calls that take each of the kernel's forms, with and without splits: rows that
+# end inside a wave's tile and inside a workgroup, sequences shorter than the
+# others, a block without a page, NaN behind the last token.
+@pytest.mark.parametrize("H,Hkv,lengths,new", [
+    (64, 1, [400], [397]), (128, 1, [2057, 2000, 1999, 700, 64], [14, 14, 14, 9, 14]),    # 128 rows
+    (64, 4, [900, 401], [600, 333]), (64, 2, [2057], [262]),                              # 256 rows
+    (32, 2, [580, 301], [267, 260]), (64, 8, [2000], [400]), (48, 1, [2171, 2100, 64, 2000, 35], [35] * 5),  # 128 rows in two groups
+    (32, 1, [69, 64, 65, 64, 66], [64] * 5), (64, 8, [2577], [22])])            # 32 rows
+def test_forms(H, Hkv, lengths, new):
+    print(f"[case] forms H={H} Hkv={Hkv} {lengths} {new}", flush=True)
+    m = Model(Hkv, len(lengths), max(lengths), seed=sum(new))
+    m.append(lengths)
+    q = m.values(sum(new), H, 0.3)
+    a = m.check_attention(new, H, q=q)
+    b = m.attend(bf16_dev(q), new, max_len=64 * m.blocks // 2)  # another plan
+    torch.cuda.synchronize()
+    m.compare(b, q, new, SCALE, "other plan")
+    gone = min(1, m.blocks - 1)
+    m.table[0, gone] = -1
+    c = m.attend(bf16_dev(q), new)
+    k, v = m.held(0)
+    L, n = lengths[0], new[0]
+    keep = [t for t in range(L) if t // BLK != gone]
+    q64 = torch.from_numpy(oracle._f32(q).astype(np.float64)).to(dev())
+    lens = torch.tensor([sum(t <= L - n + i for t in keep) for i in range(n)], device=dev())
+    for h in range(0, H, 7):
+        kk, vv = (torch.from_numpy(x[keep, h // (H // Hkv)]).to(dev()) for x in (k, v))
+        o, tol = reference(q64[:n, h], kk, vv, lens, SCALE)
+        assert ((c[:n, h].double() - o).abs() <= tol).all(), h
+    assert torch.equal(c[n:], a[n:])
