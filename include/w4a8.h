@@ -381,7 +381,9 @@ size_t w4a8_cache_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int
  *                fp32 [n_pos][64], 16-byte aligned, n_pos 1 .. 2^30
  *   q, k         either may be NULL (no heads of this kind)
  *   T            0 <= T <= W4A8_M_MAX (0: a no-op)
- * A call without a norm and without a rotation is W4A8_EINVAL.  Does not
+ * A call without a norm and without a rotation is W4A8_EINVAL.  The 8-bit
+ * cache's calls rotate by their own tables: with heads that were rotated here
+ * they take tables of one row, cos 1 and sin 0.  Does not
  * synchronize; enqueues one kernel; deterministic.
  */
 typedef struct {

@@ -219,3 +219,35 @@ def test_empty():
     got = c.run(k=k[:, :0])
     assert got[1].shape == (4, 0, D)
     c.check(got[0], None)
+
+
+def test_rotated_heads_into_the_8_bit_cache():
+    # its calls rotate by their own tables: one row of cos 1 and sin 0 leaves heads as they are
+    n, H, Hkv = 70, 8, 2
+    c = Case(n, H, Hkv, AXES[1], seed=11)
+    q, k = c.run()
+    v = c.dev[:, H + Hkv:]
+    cache = w.KVCache.empty(3, 1, Hkv)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=dev())  # noqa: E731
+    one, zero = torch.ones(1, 64, device=dev()), torch.zeros(1, 64, device=dev())
+    batch = i32([0, n]), i32([n]), i32([[2, 0]]), torch.zeros(n, dtype=torch.int32, device=dev()), one, zero
+    w.w4a8_cache_append(k, v, cache, *batch)
+    kb = to_np_bits(k.contiguous())
+    for h in range(Hkv):
+        for blk, page in ((0, 2), (1, 0)):
+            codes, s = oracle.cache_block(kb[64 * blk:64 * blk + 64, h])
+            np.testing.assert_array_equal(cache.k_codes[page, h].cpu().numpy()[:len(codes)], codes)
+            assert float(cache.scales[page, h, 0]) == s
+    o = w.w4a8_cache_attention(q, cache, *batch, D ** -0.5)
+    # the same queries over the cache's values in the plain way: 8-bit codes are exact on both sides, weights and outputs round
+    kv = [(cache.k_codes.float() * cache.scales[:, :, 0, None, None])[[2, 0]], (cache.v_codes.float() * cache.scales[:, :, 1, None, None])[[2, 0]].transpose(2, 3)]
+    kf, vf = (t.transpose(1, 2).reshape(-1, Hkv, D)[:n].double() for t in kv)
+    for h in range(H):
+        s = q[:, h].double() @ kf[:, h // 4].t().contiguous() * D ** -0.5
+        s = s.masked_fill(torch.arange(n, device=dev())[None] > torch.arange(n, device=dev())[:, None], -float("inf"))
+        p = torch.softmax(s, 1)
+        ref, b = p @ vf[:, h // 4], p @ vf[:, h // 4].abs()
+        # 16 bits of the query: |scale| top / 65024 sum |k| a score, twice that a weight; fp16 weights 2^-11, fp32 2^-14; bf16 2^-8
+        d = D ** -0.5 * q[:, h].double().abs().amax(1) / 65024 * kf[:, h // 4].abs().sum(1).max()
+        tol = 2.0 ** -8 * ref.abs() + (1 + 2.0 ** -8) * (2.0 ** -11 + 2.0 ** -14 + 2 * d[:, None] * (1 + 2 * d[:, None]) + n * 2.0 ** -37) * b + n * 2.0 ** -37 * vf.abs().max()
+        assert ((o[:, h].double() - ref).abs() <= tol).all(), h
