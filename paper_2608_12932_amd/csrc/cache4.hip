@@ -295,6 +295,9 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
     item += (split / a.S) * gridDim.z;
     split %= a.S;
   }
+  // Row blocks that see more go first: of a chunk the last ones.  (Nine ragged
+  // sequences of up to 433 tokens over up to 764 56 -> 52 us.)
+  item = (int)(gridDim.z * (gridDim.y / a.S)) - 1 - item;
 
   // ---- the workgroup's place.  A row's number wg_row0 + x is token i0 + (r0 +
   // x) / G: one division for the workgroup, and a product for the small numbers
