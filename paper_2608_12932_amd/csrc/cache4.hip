@@ -582,17 +582,18 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
     uint8_t* l_group = lds + kw * 2 * kStage;
     // A block's codes are loaded two rounds before they become operands, which
     // is a round before their use.
-    auto stage = [&](int i, const Keys& k, Values& v) {  // keys' operand (u, step) at 4 u + step, values' (h, d) at 16 + 8 h + d
+    auto stage_keys = [&](int i, const Keys& k) {  // operand (u, step) at 4 u + step
+      if (!my_keys) return;
       uint8_t* dst = l_group + (i & 1) * kStage + lane * 16 + piece * 4096;
-      if (my_keys) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + e * 1024) = keys8(word(k.codes[0], e), k.params.x);
-      }
-      if (my_values) {
-        clean_values(i, v);
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + e * 1024) = keys8(word(k.codes[0], e), k.params.x);
+    };
+    auto stage_values = [&](int i, Values& v) {  // operand (h, d) at 16 + 8 h + d
+      if (!my_values) return;
+      uint8_t* dst = l_group + (i & 1) * kStage + kStage / 2 + lane * 16 + piece * 4096;
+      clean_values(i, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + 16384 + e * 1024) = values8(word(v.codes[0], e), v.s[0], v.b[0]);
-      }
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<f16x8*>(dst + e * 1024) = values8(word(v.codes[0], e), v.s[0], v.b[0]);
     };
     auto load = [&](int page, Keys& k, Values& v) {
       if (my_keys) load_keys(page, k);
@@ -602,18 +603,24 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
     Values v[2];
     load(page0, k[0], v[0]);
     load(page1, k[1], v[1]);
-    stage(0, k[0], v[0]);
+    stage_keys(0, k[0]);
+    stage_values(0, v[0]);
     load(page2, k[0], v[0]);
     lds_barrier();
     int page3 = page_of(3);
     auto round = [&](int i, Keys& k, Values& v) {
       const int page4 = page_of(i + 4);
-      stage(i + 1, k, v);  // where block i - 1 was, which was last read before the barrier
-      load(page3, k, v);
+      // The next block's operands go where block i - 1's were, which were last read
+      // before the barrier: its values beside this block's scores, its keys beside
+      // the products with the values, vector work for either.
+      stage_values(i + 1, v);
+      if (my_values) load_values(page3, v);
       const uint8_t* src = l_group + (i & 1) * kStage + lane * 16;
       score([&](int u, int e) { return *reinterpret_cast<const f16x8*>(src + (4 * u + e) * 1024); });
       look(i, page0);
       weigh();
+      stage_keys(i + 1, k);
+      if (my_keys) load_keys(page3, k);
       add([&](int h, int d) { return *reinterpret_cast<const f16x8*>(src + (16 + 8 * h + d) * 1024); });
       lds_barrier();
       page0 = page1;
