@@ -164,10 +164,12 @@ def test_attention_rejections():
         assert call(orow=orow, oh=oh) == EINVAL, (orow, oh)
     for T, H, Hkv in ((1 << 20, 4096, 1), ((1 << 20) - 1, 4096, 8), (1 << 20, 514, 2)):
         assert call(c=cache(Hkv=Hkv), b=batch(T=T), H=H, orow=H * 128) == w.W4A8_EUNSUPPORTED, (T, H, Hkv)
-    need = w.w4a8_cache4_attention_workspace_bytes(4, 8, 32, 8, 1000)
+    # which calls are split is a matter of what they cost: 1000 long this one is not
+    # (16 blocks are four rounds of four waves, less than a merge), 4096 long it is
+    need = w.w4a8_cache4_attention_workspace_bytes(4, 8, 32, 8, 4096)
     assert need > 64 * 1024
     for ws in ((None, 0), (at(22), need - 1), (at(22, 16), need)):
-        assert call(ws=ws) == EINVAL
+        assert call(b=batch(max_blocks=64), max_len=4096, ws=ws) == EINVAL
     for over in (dict(T=0), dict(B=0)):
         assert f(cache(**NO_CACHE), batch(**NO_BATCH, **over), None, 0, 0, 32, 0.1, 1000, None, 0, 0, None, 0, None) == OK
 
