@@ -512,11 +512,7 @@ w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batc
   if (!(scale == scale) || scale > 3.4e38f || scale < -3.4e38f) return W4A8_EINVAL;  // finite
   if (batch->B == 0 || batch->T == 0) return W4A8_OK;
   if (!valid_rows(q, q_row, q_head) || !valid_rows(o, o_row, o_head)) return W4A8_EINVAL;
-  // output rows apart: heads within tokens, or tokens within heads
-  const int64_t T = batch->T, D = kCacheD;
-  if (!(((H == 1 || o_head >= D) && (T == 1 || o_row >= (H - 1) * o_head + D)) ||
-        ((T == 1 || o_row >= D) && (H == 1 || o_head >= (T - 1) * o_row + D))))
-    return W4A8_EINVAL;
+  if (!rows_apart(rows_of(o, o_row, o_head, batch->T, H))) return W4A8_EINVAL;
   if (!cache_attention_fits(a.c.T, (int)H, a.c.Hkv)) return W4A8_EUNSUPPORTED;
   a.q = {const_cast<uint16_t*>(q), q_row, q_head};
   a.o = {o, o_row, o_head};

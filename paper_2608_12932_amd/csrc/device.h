@@ -252,8 +252,8 @@ __device__ __forceinline__ uint4 ldg_nt(const uint4* p) {
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// The same for stores: what is written once and lies past what the second-level
-// caches hold, or goes to other dies' anyway, does not pass through them.
+// Streaming 16-byte store: the line does not stay in the second-level cache, from
+// which the kernel's end would have to write it back.
 __device__ __forceinline__ void stg_nt(uint4* p, uint4 v) {
   __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
 }
