@@ -268,10 +268,11 @@ constexpr float kLarge = 0x1p23f;
 //
 // 64 single tokens over 4096: 51 us, 6.0 TB/s of cache, bound by HBM and, behind
 // it, by the vector unit (384 of some 500 instructions a block turn codes into
-// fp16).  1024 tokens over 8192: 160 us, 0.86 PFLOP/s, bound by vector and matrix
-// instructions, which share a SIMD's issue: a wave's vector instructions beside
-// another's MFMAs take half of the MFMAs' time on top of their own (8 MFMAs 172
-// cycles, 32 multiply-adds 188, both together 272).
+// fp16).  1024 tokens over 8192: 145 us in a graph (0.89 PFLOP/s), 173 behind other
+// kernels in a trace, bound by vector and matrix instructions, which share a
+// SIMD's issue: a wave's vector instructions beside another's MFMAs take half of
+// the MFMAs' time on top of their own (8 MFMAs 172 cycles, 32 multiply-adds 188,
+// both together 272).
 template <int R, int KW, int NW, int AUX = kCacheDefault>
 __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnArgs a) {
   constexpr int kWaveRows = 16 * R, kSame = NW / KW, kRows = kSame * kWaveRows;
@@ -713,8 +714,9 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
 // shared forms the best would be 1.7 % slower on average and 42 % at most,
 // without the last 0.1 % and 8 %.  64 and 128 rows in four waves (one a SIMD),
 // and 16 and 32 rows in eight, tried too, took nothing off.  us of the five, at
-// its best splits each: 12 ragged sequences of up to 33 tokens over up to 1900 21
-// 19 28 36 29; 256 over 4096 - 35 41 46 38; 1024 over 8192 265 192 179 167 160.
+// its best splits each, as they are now: 12 ragged sequences of up to 33 tokens
+// over up to 1900 22 20 28 36 29; 256 over 4096 45 34 40 44 37; 1024 over 8192 277
+// 176 162 161 145.
 //   The calls were of one kind of sequence each.  A batch is taken as B
 // sequences of max_len with the average number of new tokens, so one that mixes
 // kinds (a chunk among single tokens, one long among short) gets the form and
