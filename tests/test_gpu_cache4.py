@@ -339,6 +339,32 @@ def test_every_split_gives_the_same_attention():
         m.check_attention([40], 8, max_len=max_len, label=str(max_len))
 
 
+def splits_of(B, T, H, Hkv, max_len):
+    """The splits of a call, by the partial results that its workspace holds."""
+    need = w.w4a8_cache4_attention_workspace_bytes(B, T, H, Hkv, max_len)
+    return (need - 65536) // (T * H * (D + 2) * 4) if need else 1
+
+
+@pytest.mark.parametrize("new", [[1, 1], [9, 40]])
+def test_numbers_of_splits(new):
+    # one call at the plans of lengths from one block to all of them: empty splits, one block a split, many
+    m = Model(2, 2, 12000, seed=37)
+    m.append([12000, 5000])
+    q = m.values(sum(new), 8)
+    qd, seen = bf16_dev(q), set()
+    for max_len in (64, 1300, 1700, 2300, 3000, 4500, 6000, 8000, 12000):
+        S = splits_of(2, sum(new), 8, 2, max_len)
+        if S in seen:
+            continue
+        seen.add(S)
+        print(f"[case] {new} max_len={max_len} splits={S}", flush=True)
+        out = m.attend(qd, new, max_len=max_len)
+        m.compare(out, q, new, SCALE, f"{S} splits")
+        for _ in range(5):
+            assert torch.equal(m.attend(qd, new, max_len=max_len), out), S
+    assert 1 in seen and len(seen) >= 4, seen
+
+
 @pytest.mark.parametrize("scale", [0.3, -SCALE, 0.0, -0.0, 1e-30])
 def test_scale_of_any_sign(scale):
     m = Model(2, 2, 200, seed=11)
