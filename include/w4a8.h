@@ -479,8 +479,9 @@ w4a8_status w4a8_cache4_read(const w4a8_cache4* cache, const w4a8_batch* batch, 
  * its largest exactly), its products with the keys' fp16 values are summed in
  * fp32; softmax and sums run in fp32, the softmax weights are rounded to fp16
  * for the product with the values (2^-11 relative; one below 2^-26 of the row's
- * largest, to 2^-37 of that); the output is rounded to bf16.  Scores, and scale
- * times any element of a query, have to lie within fp32's range.
+ * largest, to 2^-37 of that); the output is rounded to bf16.  Scores times
+ * log2(e), and scale times any element of a query, have to lie within fp32's
+ * range.
  *   Arguments as for w4a8_cache_attention, the batch as for w4a8_cache4_append;
  * the workspace has its own size query below.
  */

@@ -628,7 +628,7 @@ w4a8_status w4a8_cache4_attention(const w4a8_cache4* cache, const w4a8_batch* ba
   a.o = {o, o_row, o_head};
   a.H = (int)H;
   // as in w4a8_stream_attention, the queries carry the scale's sign, or its zero
-  a.scale_log2e = (scale == 0.0f ? 1.0f : std::fabs(scale)) * 1.4426950408889634f;
+  a.scale = scale == 0.0f ? 1.0f : std::fabs(scale);
   a.q_sign = scale == 0.0f ? 0.0f : scale < 0.0f ? -1.0f : 1.0f;
   a.max_len = (int)max_len;
   hipError_t error;

@@ -35,7 +35,7 @@ struct Cache4AttnArgs {
   Cache4Batch c;
   TokenRows q, o;
   int H, G;               // query heads, and how many share a kv head
-  float scale_log2e;      // |score scale| times log2(e)
+  float scale;            // |score scale| (1 for a scale of 0)
   float q_sign;           // the scale's sign, 0 for a scale of 0
   int max_len;            // the longest sequence, for the choice of splits alone
   // set by the launcher

@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256) void cache4_read(const Cache4RowsArgs a) {
 // more than 3, so that the sums are hardly ever rescaled: weights reach 2^15,
 // and fp16 holds those down to 2^-14, 2^-26 of the largest, in full precision,
 // smaller ones to 2^-24.
-constexpr float kWeightShift = 12.0f, kSlack = 3.0f;
+constexpr float kWeightShift = 12.0f, kSlack = 3.0f, kLog2e = 1.4426950408889634f;
 // A score's exponent is one multiply-add, score factor - offset.  From here on
 // its rounding to fp32 could lift it past fp16's range: there the offset is the
 // rounded score itself and is subtracted from rounded scores.
@@ -358,7 +358,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
                             f16x2_bits(bf16_lo(w[4 * e + 1]) * to, bf16_hi(w[4 * e + 1]) * to),
                             f16x2_bits(bf16_lo(w[4 * e + 2]) * to, bf16_hi(w[4 * e + 2]) * to),
                             f16x2_bits(bf16_lo(w[4 * e + 3]) * to, bf16_hi(w[4 * e + 3]) * to)));
-    f[t] = fmaxf(__uint_as_float((uint32_t)(127 - up) << 23) * a.scale_log2e, 0x1p-126f);  // above 0: a masked -inf stays
+    // the row's power of two first: the scale times log2(e) may lie past fp32; above 0: a masked -inf stays
+    f[t] = fmaxf(__uint_as_float((uint32_t)(127 - up) << 23) * a.scale * kLog2e, 0x1p-126f);
     last_key[t] = wg_row0 + x < n_rows ? s.len - s.n + i : -1;
   }
 

@@ -372,6 +372,18 @@ def test_scale_of_any_sign(scale):
     m.check_attention([1, 20], 8, scale=scale)
 
 
+@pytest.mark.parametrize("scale", [2.3e38, 2.4e38, 3.3e38, -3.3e38])
+@pytest.mark.parametrize("n", [1, 40])
+def test_scales_near_the_largest(n, scale):
+    # |scale| log2(e) passes fp32 from 2.36e38 on; scale times the queries' elements does not
+    m = Model(2, 1, 200, seed=38)
+    m.append([200])
+    q = I.to_bf16_bits((oracle._f32(m.values(n, 8, 0.3)) * np.float32(2.0 ** -128)).astype(np.float32))  # subnormal, in steps of 2^-133
+    q[:, 3] = 0  # every token counts alike
+    assert np.abs(oracle._f32(q).astype(np.float64) * scale).max() < 2.0 ** 7
+    m.check_attention([n], 8, scale=scale, q=q)
+
+
 def test_rows_that_see_nothing():
     m = Model(2, 3, 100, seed=12)
     m.append([100, 5, 20])
