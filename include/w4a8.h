@@ -370,7 +370,7 @@ size_t w4a8_cache_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int
  *                in multiples of 8.  out is x itself with x's strides (in
  *                place), or apart from both kinds' inputs and from the other's
  *                output (W4A8_EINVAL where that cannot be seen from two equal
- *                strides or disjoint ranges); its rows must not overlap each
+ *                strides, the strides' common divisor or disjoint ranges); its rows must not overlap each
  *                other, nor any other argument
  *   heads        0 .. 4096 (0: none of this kind, its pointers are not read)
  *   gamma        device, bf16 gain [128], 16-byte aligned, or NULL: no norm
@@ -483,7 +483,9 @@ w4a8_status w4a8_cache4_read(const w4a8_cache4* cache, const w4a8_batch* batch, 
  * log2(e), and scale times any element of a query, have to lie within fp32's
  * range.
  *   Arguments as for w4a8_cache_attention, the batch as for w4a8_cache4_append;
- * the workspace has its own size query below.
+ * the workspace has its own size query below.  Output rows over q or over the
+ * cache are W4A8_EINVAL, also where what w4a8_qk_norm_rope and w4a8_cache4_read
+ * look at does not show that they are apart.
  */
 w4a8_status w4a8_cache4_attention(const w4a8_cache4* cache, const w4a8_batch* batch, const uint16_t* q, int64_t q_row,
                                   int64_t q_head, int64_t H, float scale, int64_t max_len, uint16_t* o, int64_t o_row,

@@ -932,10 +932,11 @@ def w4a8_cache4_attention(q: torch.Tensor, cache: KVCache4, starts: torch.Tensor
                           workspace: Workspace | torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Attention of a step's new tokens over the 4-bit cache that holds them
     already (w4a8_cache4_append): q bf16 [T][H][128] (rotated already), strided
-    views allowed -> bf16 [T][H][128] (`out` may be a strided view too; rows of
-    no sequence are not written).  New token i of n of a sequence of length L
-    sees its tokens up to L - n + i.  max_len, an upper bound of the lengths (the
-    table's by default), only decides how the work is split."""
+    views allowed -> bf16 [T][H][128] (`out` may be a strided view too, apart
+    from q and the cache; rows of no sequence are not written).  New token i of n
+    of a sequence of length L sees its tokens up to L - n + i.  max_len, an upper
+    bound of the lengths (the table's by default), only decides how the work is
+    split."""
     if stream is None:
         buf, home, own = _workspace_of(workspace)
         r = (_fast or _load_fast()).cache4_attention(q, cache, starts, lengths, table, scale, max_len, out, buf, home, own)

@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdio>
 #include <mutex>
+#include <numeric>
 
 #include "attention.h"
 #include "cache.h"
@@ -261,7 +262,8 @@ bool rows_apart(const Rows& a) {
          ((a.T == 1 || a.row >= D) && (a.heads == 1 || a.head >= (a.T - 1) * a.row + D));
 }
 // Two sets of rows that share no element, as far as that can be seen: disjoint
-// ranges, or equal strides with one set's places in the other's gaps.
+// ranges, equal strides with one set's places in the other's gaps, or places that
+// differ by the strides' common divisor's remainder (every other head of a matrix).
 bool rows_disjoint(const Rows& a, const Rows& b) {
   if (!overlap(a.p, (size_t)a.extent() * 2, b.p, (size_t)b.extent() * 2)) return true;
   auto in_gaps = [&](int64_t stride, int64_t a_span, int64_t b_span) {
@@ -272,6 +274,8 @@ bool rows_disjoint(const Rows& a, const Rows& b) {
   if (a.T > 1 && b.T > 1 && a.row == b.row && a.row > 0 &&
       in_gaps(a.row, (a.heads - 1) * a.head + kCacheD, (b.heads - 1) * b.head + kCacheD))
     return true;
+  const int64_t unit = std::gcd(std::gcd(a.T > 1 ? a.row : 0, a.heads > 1 ? a.head : 0), std::gcd(b.T > 1 ? b.row : 0, b.heads > 1 ? b.head : 0));
+  if (unit > 0 && in_gaps(unit, kCacheD, kCacheD)) return true;
   return a.heads > 1 && b.heads > 1 && a.head == b.head && a.head > 0 &&
          in_gaps(a.head, (a.T - 1) * a.row + kCacheD, (b.T - 1) * b.row + kCacheD);
 }
@@ -622,8 +626,10 @@ w4a8_status w4a8_cache4_attention(const w4a8_cache4* cache, const w4a8_batch* ba
   if (!(scale == scale) || scale > 3.4e38f || scale < -3.4e38f) return W4A8_EINVAL;  // finite
   if (batch->B == 0 || batch->T == 0) return W4A8_OK;
   if (!valid_rows(q, q_row, q_head) || !valid_rows(o, o_row, o_head)) return W4A8_EINVAL;
-  if (!rows_apart(rows_of(o, o_row, o_head, batch->T, H))) return W4A8_EINVAL;
+  const Rows in = rows_of(q, q_row, q_head, batch->T, H), out = rows_of(o, o_row, o_head, batch->T, H);
+  if (!rows_apart(out)) return W4A8_EINVAL;
   if (!cache_attention_fits(a.c.T, (int)H, a.c.Hkv)) return W4A8_EUNSUPPORTED;
+  if (!rows_disjoint(out, in) || !apart_from_cache(out, cache)) return W4A8_EINVAL;
   a.q = {const_cast<uint16_t*>(q), q_row, q_head};
   a.o = {o, o_row, o_head};
   a.H = (int)H;

@@ -174,6 +174,22 @@ def test_attention_rejections():
         assert f(cache(**NO_CACHE), batch(**NO_BATCH, **over), None, 0, 0, 32, 0.1, 1000, None, 0, 0, None, 0, None) == OK
 
 
+def test_attention_output_over_inputs():
+    # T 8, H 32, q a view of a fused projection's rows: over q, in its gaps but not far enough, over the cache
+    f = w.lib().w4a8_cache4_attention
+    call = lambda q=at(20), qr=6144, qh=128, o=at(21), orow=4096, oh=128, T=8, H=32: f(  # noqa: E731
+        cache(), batch(T=T), q, qr, qh, H, 0.1, 1000, o, orow, oh, at(22), 1 << 30, None)
+    for over in (dict(o=at(20), orow=6144), dict(o=at(20)), dict(o=at(20), qr=4096), dict(o=at(20, 2 * 7 * 6144), orow=6144),
+                 dict(o=at(20, 2 * (4096 - 8)), orow=6144), dict(o=at(20, 2 * (6144 - 4096)), orow=6144),
+                 dict(q=at(21, 2 * (7 * 4096 + 31 * 128 + 120))), dict(q=at(21), qr=0, qh=0),  # one row for all
+                 dict(q=at(20), qr=128, qh=1024, o=at(20, 2 * 1024), orow=128, oh=1024), dict(T=1, o=at(20, 2 * 128 * 31))):
+        assert call(**over) == EINVAL, over
+    for i, n in enumerate((4096, 4096, 512, 512)):  # codes, codes, parameters, parameters of a page's head
+        for off in (0, 10 * 8 * n - 16):
+            assert call(o=at(i, off)) == EINVAL, (i, off)
+        assert call(o=P(((i + 1) << 32) - 16)) == EINVAL, i
+
+
 def test_workspace_bytes():
     f = w.w4a8_cache4_attention_workspace_bytes
     assert f(64, 64, 32, 8, 64) == 0  # one block: nothing to split

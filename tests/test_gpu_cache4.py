@@ -561,6 +561,40 @@ def test_layouts_of_queries_and_output():
     assert torch.equal(o.transpose(0, 1), want)
 
 
+def test_read_into_every_other_head():
+    m = Model(2, 1, 100, seed=43).append([100])
+    want = read(m, [100])
+    both = torch.zeros(100, 4, D, dtype=torch.bfloat16, device=dev())
+    got = read(m, [100], k_out=both[:, ::2], v_out=both[:, 1::2])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_output_beside_the_queries():
+    # one matrix's rows, halves of a token or every other head; over the queries or the cache is refused
+    m = Model(2, 2, 300, seed=39)
+    m.append([300, 90])
+    for new in ([9, 30], [1, 0]):
+        T, H = sum(new), 8
+        q = m.values(T, H)
+        want = m.check_attention(new, H, q=q)
+        for both in (torch.zeros(T, 2 * H, D, dtype=torch.bfloat16, device=dev()), torch.zeros(2 * H, T, D, dtype=torch.bfloat16, device=dev()).transpose(0, 1)):
+            for qd, o in ((both[:, :H], both[:, H:]), (both[:, H:], both[:, :H]), (both[:, ::2], both[:, 1::2]), (both[:, 1::2], both[:, ::2])):
+                qd.copy_(bf16_dev(q))
+                o.zero_()
+                m.attend(qd, new, out=o)
+                assert torch.equal(o, want) and torch.equal(qd, bf16_dev(q))
+        both = torch.cat([bf16_dev(q), bf16_dev(q)], 1)
+        before, pages = both.clone(), [t.clone() for t in m.cache]
+        flat = m.cache.k_codes.view(-1).view(torch.bfloat16)
+        for qd, o in ((both[:, :H], both[:, :H]), (both[:, :H], both[:, 1:H + 1]), (both[:, H:], both[:, H - 1:-1]),
+                      (both[:, :H], flat[-T * H * D:].view(T, H, D))):
+            for kw in (dict(), dict(stream=torch.cuda.current_stream())):
+                with pytest.raises(w.W4A8Error):
+                    m.attend(qd, new, out=o, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(both, before) and all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(m.cache, pages))
+
+
 def test_shared_pages():
     # two sequences with a common beginning
     m = Model(2, 2, 200, seed=23)

@@ -94,6 +94,19 @@ def test_without_a_norm_or_a_rotation(T):
     c.check(q, None)
 
 
+def test_every_other_head():
+    # inputs and outputs take turns in one matrix
+    c = Case(70, 6, 6, AXES[1], seed=14)
+    want = c.run()
+    both = torch.zeros(70, 24, D, dtype=torch.bfloat16, device=dev())
+    views = [both[:, i::4] for i in range(4)]
+    for x, v in zip(c.views(), views):
+        v.copy_(x)
+    c.run(q=views[0], k=views[1], q_out=views[2], k_out=views[3])
+    for a, b in zip(views, (*c.views(), *want)):
+        assert torch.equal(a, b)
+
+
 def test_in_place_and_strided_outputs():
     c = Case(70, 12, 4, AXES[1], seed=4)
     want = c.run()
