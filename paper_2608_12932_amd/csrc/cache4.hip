@@ -79,7 +79,7 @@ constexpr int64_t kResident = 256 * 8;  // workgroups of 256 threads that the ch
 template <int N>
 __global__ __launch_bounds__(256) void cache4_append(const Cache4RowsArgs a) {
   constexpr int kPitch = kD + 4;  // bytes of a token's codes in LDS, off the banks' period
-  __shared__ uint8_t l_codes[N][kEight * kPitch];
+  __shared__ __align__(16) uint8_t l_codes[N][kEight * kPitch];
   const Cache4Batch& cb = a.c;
   const int tid = threadIdx.x & 127, h0 = blockIdx.y * N;
   const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7) == 0;
