@@ -533,7 +533,7 @@ w4a8_status w4a8_cache_attention(const w4a8_cache* cache, const w4a8_batch* batc
 w4a8_status w4a8_qk_norm_rope(const w4a8_heads* q, const w4a8_heads* k, int64_t T, float eps, const w4a8_rope* rope,
                               hipStream_t stream) {
   if (T < 0 || T > W4A8_M_MAX) return W4A8_EINVAL;
-  if (!(eps > 0.0f) || !(eps <= 3.4e38f)) return W4A8_EINVAL;  // also rejects NaN and inf
+  if (!(eps > 0.0f) || !std::isfinite(eps)) return W4A8_EINVAL;
   const w4a8_heads* kinds[2] = {q && q->heads ? q : nullptr, k && k->heads ? k : nullptr};
   for (const w4a8_heads* h : kinds)
     if (h && (h->heads < 0 || h->heads > kCacheHeadsMax || (!h->gamma && !rope))) return W4A8_EINVAL;
@@ -623,7 +623,7 @@ w4a8_status w4a8_cache4_attention(const w4a8_cache4* cache, const w4a8_batch* ba
   if (!valid_cache_attention(batch->B, batch->T, H, cache->Hkv, max_len) ||
       max_len > batch->max_blocks * W4A8_CACHE_BLOCK)
     return W4A8_EINVAL;
-  if (!(scale == scale) || scale > 3.4e38f || scale < -3.4e38f) return W4A8_EINVAL;  // finite
+  if (!std::isfinite(scale)) return W4A8_EINVAL;
   if (batch->B == 0 || batch->T == 0) return W4A8_OK;
   if (!valid_rows(q, q_row, q_head) || !valid_rows(o, o_row, o_head)) return W4A8_EINVAL;
   const Rows in = rows_of(q, q_row, q_head, batch->T, H), out = rows_of(o, o_row, o_head, batch->T, H);

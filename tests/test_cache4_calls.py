@@ -174,6 +174,14 @@ def test_attention_rejections():
         assert f(cache(**NO_CACHE), batch(**NO_BATCH, **over), None, 0, 0, 32, 0.1, 1000, None, 0, 0, None, 0, None) == OK
 
 
+def test_the_largest_finite_numbers_are_taken():
+    top = float(np.finfo(np.float32).max)
+    for scale in (top, -top, 3.401e38):
+        assert w.lib().w4a8_cache4_attention(cache(), batch(T=0), None, 0, 0, 32, scale, 1000, None, 0, 0, None, 0, None) == OK
+    for eps in (top, 3.401e38):
+        assert norm_rope(T=0, eps=eps) == OK
+
+
 def test_attention_output_over_inputs():
     # T 8, H 32, q a view of a fused projection's rows: over q, in its gaps but not far enough, over the cache
     f = w.lib().w4a8_cache4_attention
