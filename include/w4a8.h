@@ -363,8 +363,8 @@ size_t w4a8_cache_attention_workspace_bytes(int64_t B, int64_t T, int64_t H, int
  * for the pairs i = d < 64, with cos_i = rope_cos[p][i], sin_i = rope_sin[p][i]
  * and p = pos[axis[i]][t]: positions may have several axes (time, height and
  * width of an image's or video's tokens), each of which turns its own pairs.
- * fp32 throughout, rounded once, to bf16.  The mean square has to be finite in
- * fp32.
+ * fp32 throughout, rounded once, to bf16.  The mean square plus eps has to lie
+ * between 2^-100 and fp32's largest number.
  *   x, out       device, bf16, 16-byte aligned: token t, head h at t * row + h *
  *                head elements (out: out_row, out_head), 128 in a row; strides
  *                in multiples of 8.  out is x itself with x's strides (in
@@ -479,9 +479,10 @@ w4a8_status w4a8_cache4_read(const w4a8_cache4* cache, const w4a8_batch* batch, 
  * its largest exactly), its products with the keys' fp16 values are summed in
  * fp32; softmax and sums run in fp32, the softmax weights are rounded to fp16
  * for the product with the values (2^-11 relative; one below 2^-26 of the row's
- * largest, to 2^-37 of that); the output is rounded to bf16.  Scores times
- * log2(e), and scale times any element of a query, have to lie within fp32's
- * range.
+ * largest, to 2^-37 of that, or, where the row's largest score times log2(e) is
+ * 2^23 or more in magnitude, one below 2^-14 of the largest, to 2^-25 of that);
+ * the output is rounded to bf16.  Scores times log2(e), and scale times any
+ * element of a query, have to lie within fp32's range.
  *   Arguments as for w4a8_cache_attention, the batch as for w4a8_cache4_append;
  * the workspace has its own size query below.  Output rows over q or over the
  * cache are W4A8_EINVAL, also where what w4a8_qk_norm_rope and w4a8_cache4_read
