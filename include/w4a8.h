@@ -333,7 +333,9 @@ w4a8_status w4a8_cache_append(const w4a8_cache* cache, const w4a8_batch* batch, 
  *                otherwise)
  *   scale        finite, of either sign or 0
  *   max_len      an upper bound of the lengths, 1 .. 64 max_blocks: it decides
- *                how the work is split, and bounds nothing else
+ *                how the work is split, alike for all sequences (those much
+ *                longer than the others, or with many more new tokens, are
+ *                faster in a call of their own), and bounds nothing else
  *   o            device, bf16: token t, head h at t * o_row + h * o_head
  *                elements; the rows must not overlap each other (W4A8_EINVAL)
  *                or an input

@@ -904,7 +904,9 @@ def w4a8_cache4_read(cache: KVCache4, starts: torch.Tensor, lengths: torch.Tenso
     """Tokens of the 4-bit cache back as (k, v) bf16 [rows][Hkv][128]: rows
     starts[b] .. starts[b + 1] - 1 are the last of the lengths[b] tokens that
     sequence b holds.  k_out, v_out take the results and may be strided views
-    (also of [Hkv][rows][128], transposed); rows of no sequence are not written."""
+    (also of [Hkv][rows][128], transposed).  Rows of no sequence are not written,
+    nor are a sequence's rows before its first token, where it has more rows than
+    tokens: in outputs that the call allocates they hold anything."""
     if stream is None:
         r = (_fast or _load_fast()).cache4_read(cache, starts, lengths, table, rows, k_out, v_out)
         if r is not None:
@@ -936,7 +938,10 @@ def w4a8_cache4_attention(q: torch.Tensor, cache: KVCache4, starts: torch.Tensor
     from q and the cache; rows of no sequence are not written).  New token i of n
     of a sequence of length L sees its tokens up to L - n + i.  max_len, an upper
     bound of the lengths (the table's by default), only decides how the work is
-    split."""
+    split, alike for all sequences: by their number, the average number of new
+    tokens and max_len.  Sequences much longer than the others, or with many more
+    new tokens, are faster in a call of their own (one of 100000 tokens beside 63
+    of 1000: 495 us in one call, 45 in two)."""
     if stream is None:
         buf, home, own = _workspace_of(workspace)
         r = (_fast or _load_fast()).cache4_attention(q, cache, starts, lengths, table, scale, max_len, out, buf, home, own)

@@ -288,8 +288,9 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const int G = a.G, kw = wave / kSame, same = wave % kSame;
-  // Workgroups of neighbouring kv heads go to the XCDs in turn, so that all of
-  // a head's row blocks find its pages in one L2.
+  // Workgroups of neighbouring kv heads go to the XCDs in turn, so that with a
+  // multiple of 8 of them all of a head's row blocks find its pages in one L2 (with
+  // 4 in two, with an odd number in all).
   const int hk = blockIdx.x;
   int split = blockIdx.y, item = blockIdx.z;
   if ((int)gridDim.y > a.S) {  // more row blocks than one axis of a launch holds
@@ -720,8 +721,11 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
 // 176 162 161 145.
 //   The calls were of one kind of sequence each.  A batch is taken as B
 // sequences of max_len with the average number of new tokens, so one that mixes
-// kinds (a chunk among single tokens, one long among short) gets the form and
-// splits of neither: a call for each kind is faster.
+// kinds gets the form and splits of neither, and a call for each kind is faster:
+// one token each of 63 sequences of 1000 and one of 100000, 32 heads on 8: 495 us
+// in one call (no splits), 17 + 28 in two; 63 single tokens beside a chunk of 1024,
+// all over 8192: 313, 96 + 144.  Beside a chunk of 512 over 4096, 16 heads on 16, it
+// makes no difference: 138, 99 + 37.
 typedef void (*Attn4Fn)(const Cache4AttnArgs);
 struct Attn4Form {
   int rows, KW, threads;
@@ -736,9 +740,10 @@ const Attn4Form kForms[] = {
     {128, 2, 512, 7240, 830, 5420, 2310, cache4_attention<2, 2, 8>},
 };
 constexpr int64_t kMergeCost = 3430, kMergePart = 24;  // ns, ns for 100 (split, token, head)
-// Where the rows of a sequence's kv head are one row block, its pages are read
-// once, past the caches: of 13 calls from 1 MB to 300 MB none was slower so, and
-// 64 sequences of 4096 take 51 us instead of 63.
+// Where the rows of an average sequence's kv head are one row block, pages are read
+// past the caches, as each is read once: of 13 calls from 1 MB to 300 MB none was
+// slower so, and 64 sequences of 4096 take 51 us instead of 63.  (A longer chunk
+// among single tokens reads its pages so once for each of its row blocks.)
 const Attn4Fn kStreamFn = cache4_attention<1, 4, 4, kCacheStream>;
 constexpr int64_t kMaxAxis = 65535;  // workgroups along the second and third axis of a launch
 
