@@ -544,6 +544,80 @@ def test_arrays_out_of_range_reach_no_other_memory():
         assert out.shape == q.shape and torch.equal(before, m.cache.k_codes)
 
 
+OUT_OF_RANGE = [([-5, 3, 1, 400], [1 << 30, -7, 90]), ([0, 20, 20, 20], [0, 0, 0]), ([9, 2, 30, 5], [100, 1, 2]), ([0, 0, 0, 0], [5, 5, 5]),
+                ([0, 7, 7, 20], [-(1 << 31), (1 << 31) - 1, 1 << 30]), ([-(1 << 31), (1 << 31) - 1, 0, 20], [200, 100, 50])]
+
+
+@pytest.mark.parametrize("starts,lengths", OUT_OF_RANGE)
+def test_arrays_out_of_range_leave_the_rest_alone(starts, lengths):
+    m = Model(2, 3, 200, seed=44, pages=3 * 4 + 9)
+    m.append([200, 100, 50])
+    q, kv = bf16_dev(m.values(20, 8)), bf16_dev(m.values(20, 2))
+    s, n, none = i32(starts), i32(lengths), i32(np.full_like(m.table, -1))
+    rows = lambda H: torch.full((36, H, D), 9.0, dtype=torch.bfloat16, device=dev())  # noqa: E731
+    out, k, v = rows(8), rows(2), rows(2)
+    same = lambda a, b: torch.equal(a.view(torch.int16), b.view(torch.int16))  # noqa: E731
+    before = [t.clone() for t in m.cache]
+    print(f"[case] {starts} {lengths}", flush=True)
+    for table in (i32(m.table), none):
+        w.w4a8_cache4_attention(q, m.cache, s, n, table, SCALE, out=out[8:28])
+        w.w4a8_cache4_read(m.cache, s, n, table, 20, k_out=k[8:28], v_out=v[8:28])
+    w.w4a8_cache4_append(kv, kv, m.cache, s, n, none)
+    torch.cuda.synchronize()
+    for t in (out, k, v):
+        assert (t[:8] == 9).all() and (t[28:] == 9).all()
+    assert all(same(a, b) for a, b in zip(before, m.cache))
+    # with pages, tokens may be held there, and nowhere else
+    w.w4a8_cache4_append(kv, kv, m.cache, s, n, i32(m.table))
+    torch.cuda.synchronize()
+    others = [p for p in range(21) if p not in m.table]
+    assert all(same(a[others], b[others]) for a, b in zip(before, m.cache))
+
+
+@pytest.mark.parametrize("kind", ["k", "v"])
+def test_read_of_one_kind(kind):
+    # the library's call with no room for the other: its rows come as with both
+    m = Model(3, 2, 100, seed=45).append([70, 20])
+    want = dict(zip("kv", read(m, [70, 20])))
+    out = torch.full((90, 3, D), 7.0, dtype=torch.bfloat16, device=dev())
+    starts, lengths, table = m.batch([70, 20])
+    c, _ = w._cache4_args(m.cache)
+    b = w._batch4_args(90, starts, lengths, table)
+    args = dict(k=(None, 0, 0), v=(None, 0, 0))
+    args[kind] = (out.data_ptr(), out.stride(0), out.stride(1))
+    assert w.lib().w4a8_cache4_read(c, b, *args["k"], *args["v"], torch.cuda.current_stream().cuda_stream) == w.W4A8_OK
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[kind])
+
+
+@pytest.mark.parametrize("L", [300, 5000])
+def test_pages_past_the_caches_and_through_them(L):
+    # Three new tokens of 8 heads are 24 rows, more than the 16 of a workgroup: pages through the caches.  The same
+    # tokens as a sequence each, on the same pages, are 8 rows: past them.  Splits and the order of sums are alike, and
+    # tokens that a row does not see add 0, so the bits are the same.
+    m = Model(1, 1, L, seed=46)
+    m.append([L])
+    q = m.values(3, 8)
+    want = m.check_attention([3], 8, q=q)
+    got = w.w4a8_cache4_attention(bf16_dev(q), m.cache, i32(range(4)), i32([L - 2, L - 1, L]), i32(np.tile(m.table, (3, 1))), SCALE)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("H,Hkv,lengths,new", [(32, 8, [300] * 40 + [20000] + [77] * 23, [1] * 64), (16, 16, [500] * 30 + [900] + [64], [1] * 30 + [300, 1])])
+def test_sequences_unlike_each_other(H, Hkv, lengths, new):
+    # one long sequence among short ones, a chunk among single tokens
+    B, blocks = len(lengths), [-(-L // BLK) for L in lengths]
+    at = np.cumsum([0] + blocks)
+    m = Model(Hkv, 1, BLK, seed=47, pages=int(at[-1]) + 3)
+    m.B, m.blocks, m.table = B, max(blocks), np.full((B, max(blocks)), -1, np.int32)  # pages for what each holds
+    m.k, m.v = ([np.zeros((0, Hkv, D), np.uint16) for _ in range(B)] for _ in range(2))
+    pages = m.rng.permutation(at[-1])
+    for b in range(B):
+        m.table[b, :blocks[b]] = pages[at[b]:at[b + 1]]
+    m.append(lengths)
+    m.check_attention(new, H, workspace=w.Workspace())
+
+
 def test_layouts_of_queries_and_output():
     m = Model(2, 2, 300, seed=22)
     m.append([300, 90])
