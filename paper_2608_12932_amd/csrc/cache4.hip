@@ -271,8 +271,9 @@ constexpr float kLarge = 0x1p23f;
 // fp16).  1024 tokens over 8192: 145 us in a graph (0.89 PFLOP/s), 173 behind other
 // kernels in a trace, bound by vector and matrix instructions, which share a
 // SIMD's issue: a wave's vector instructions beside another's MFMAs take half of
-// the MFMAs' time on top of their own (8 MFMAs 172 cycles, 32 multiply-adds 188,
-// both together 272).
+// the MFMAs' time on top of their own (8 MFMAs 175 cycles, 32 multiply-adds 189,
+// both together 278).  Some of the vector work is done over: each of a head's row
+// blocks (32 of 128 rows there) turns the same codes into fp16.
 template <int R, int KW, int NW, int AUX = kCacheDefault>
 __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnArgs a) {
   constexpr int kWaveRows = 16 * R, kSame = NW / KW, kRows = kSame * kWaveRows;
@@ -711,10 +712,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache4_attention(const Cache4AttnA
 // full chip each of the ceil(workgroups / 256) that a CU runs adds thr +
 // thr_round a round.  Fitted, with the merge's 3430 + 0.24 a (split, token,
 // head), to 95 calls (B 1 - 64, 1 - 1024 new tokens, 60 - 90000 long, five head
-// layouts) at up to 12 numbers of splits: what the rule picks is 0.1 % above the
-// best of all forms and splits on average, 2 % at most.  Without the three
-// shared forms the best would be 1.7 % slower on average and 42 % at most,
-// without the last 0.1 % and 8 %.  64 and 128 rows in four waves (one a SIMD),
+// layouts) at up to 12 numbers of splits: what the rule picks is 0.2 % above the
+// best of all forms and splits on average, 6 % at most.  Without the three
+// shared forms the best would be 1.9 % slower on average and 39 % at most,
+// without the last 0.2 % and 15 %.  64 and 128 rows in four waves (one a SIMD),
 // and 16 and 32 rows in eight, tried too, took nothing off.  us of the five, at
 // its best splits each, as they are now: 12 ragged sequences of up to 33 tokens
 // over up to 1900 22 20 28 36 29; 256 over 4096 45 34 40 44 37; 1024 over 8192 277
@@ -741,9 +742,11 @@ const Attn4Form kForms[] = {
 };
 constexpr int64_t kMergeCost = 3430, kMergePart = 24;  // ns, ns for 100 (split, token, head)
 // Where the rows of an average sequence's kv head are one row block, pages are read
-// past the caches, as each is read once: of 13 calls from 1 MB to 300 MB none was
-// slower so, and 64 sequences of 4096 take 51 us instead of 63.  (A longer chunk
-// among single tokens reads its pages so once for each of its row blocks.)
+// past the caches, as each is read once: of 13 calls from 1 MB to 300 MB, on another
+// cache each time (another layer's), none was slower so, and 64 sequences of 4096
+// take 52 us instead of 61.  On the same cache again, of which the memory-side one
+// still holds some, two from 150 MB on were (29.3 -> 31.0 us, 55 -> 60).  A longer
+// chunk among single tokens reads its pages so once for each of its row blocks.
 const Attn4Fn kStreamFn = cache4_attention<1, 4, 4, kCacheStream>;
 constexpr int64_t kMaxAxis = 65535;  // workgroups along the second and third axis of a launch
 
