@@ -266,7 +266,7 @@ constexpr float kLarge = 0x1p23f;
 // wave into fp16 operands and hands them round through LDS, a block ahead of
 // their use; operand order, 1 KiB an operand, so no access meets a bank twice.
 //
-// 64 single tokens over 4096: 51 us, 6.0 TB/s of cache, bound by HBM and, behind
+// 64 single tokens over 4096: 51 us, 5.9 TB/s of cache, bound by HBM and, behind
 // it, by the vector unit (384 of some 500 instructions a block turn codes into
 // fp16).  1024 tokens over 8192: 145 us in a graph (0.89 PFLOP/s), 173 behind other
 // kernels in a trace, bound by vector and matrix instructions, which share a
